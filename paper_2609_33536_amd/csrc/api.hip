@@ -12,6 +12,7 @@
 
 #include "ekv.h"
 #include "common.h"
+#include "host_checks.h"
 #include "host_status.h"
 #include "launch.h"
 
@@ -33,16 +34,14 @@ ekv_status fail(ekv_status s, const char* fmt, ...) {
 
 }  // namespace ekv
 
-namespace {
-
-using ekv::fail;
+namespace ekv {
 
 ekv_status hip_status(hipError_t e, const char* what) {
   if (e == hipSuccess) return EKV_OK;
   return fail(EKV_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
-bool supported_group(int g) { return g == 1 || g == 2 || g == 4 || g == 8 || g == 16; }
+static bool supported_group(int g) { return g == 1 || g == 2 || g == 4 || g == 8 || g == 16; }
 
 ekv_status check_pool(const ekv_pool* p) {
   if (!p) return fail(EKV_ERR_INVALID, "pool is NULL");
@@ -82,6 +81,19 @@ int max_seq_blocks(const ekv_batch* b) {
   const int len = b->max_seq_len > 0 ? b->max_seq_len : b->max_blocks * ekv::kPage;
   return (len + ekv::kPage - 1) / ekv::kPage;
 }
+
+float log2e_scale(float scale) { return scale * 1.4426950408889634f; }
+
+bool debug_mode() {
+  const char* e = getenv("EKV_DEBUG");
+  return e && e[0] && strcmp(e, "0") != 0;
+}
+
+}  // namespace ekv
+
+namespace {
+
+using namespace ekv;
 
 // Fewest pairs (32 tokens) one workgroup streams: 1 / 32 of the longest
 // sequence's pairs, at most 8.  A workgroup alone takes ~1.5 us a pair, so a
@@ -212,8 +224,6 @@ ekv_status scratch_address(void** out) {
   return EKV_OK;
 }
 
-float log2e_scale(float scale) { return scale * 1.4426950408889634f; }
-
 // ---- device-side validation and the EKV_DEBUG mode ------------------------
 
 const char* violation_name(int k) {
@@ -223,11 +233,6 @@ const char* violation_name(int k) {
       "mode or boundaries disagree with the tags", "list pair out of range", "list pair in the wrong state",
       "list pair not two full blocks", "list pair listed twice", "new block out of range, repeated or in use"};
   return k >= 0 && k < EKV_VIOL_COUNT ? names[k] : "unknown";
-}
-
-bool debug_mode() {
-  const char* e = getenv("EKV_DEBUG");
-  return e && e[0] && strcmp(e, "0") != 0;
 }
 
 ekv_status check_validate_batch(const ekv_pool* pool, const ekv_batch* batch, int32_t* report) {
@@ -285,7 +290,9 @@ ekv_status debug_verdict(const int32_t* report, hipStream_t stream, const char* 
   return EKV_OK;
 }
 
-ekv_status debug_check_batch(const ekv_pool* pool, const ekv_batch* batch, hipStream_t stream, const char* call) {
+}  // namespace
+
+ekv_status ekv::debug_check_batch(const ekv_pool* pool, const ekv_batch* batch, hipStream_t stream, const char* call) {
   if ((long long)batch->batch * batch->max_blocks >= (1LL << 31))
     return fail(EKV_ERR_UNSUPPORTED, "%s (EKV_DEBUG): batch * max_blocks must be below 2^31", call);
   int32_t* report = nullptr;
@@ -295,6 +302,8 @@ ekv_status debug_check_batch(const ekv_pool* pool, const ekv_batch* batch, hipSt
     return st;
   return debug_verdict(report, stream, call);
 }
+
+namespace {
 
 ekv_status debug_check_list(const ekv_pool* pool, int kind, int n, const int32_t* pairs, const int32_t* new_blocks,
                             const int32_t* block_table, const uint8_t* tags, int batch, int max_blocks,

@@ -567,6 +567,171 @@ ekv_status ekv_ctrl_promotion(const ekv_ctrl_config* cfg, ekv_ctrl_state* st, in
                               int32_t max_blocks, int32_t page_size, int32_t* h_pairs_out, int32_t max_pairs,
                               int32_t* n_out);
 
+/*
+ * ---- The serving step around the cache ------------------------------------
+ *
+ * What a decode or prefill step does besides attention, on the GPU and
+ * without the host: find cache room for the new tokens (ekv_extend), turn
+ * queries and keys by their positions and store the new K and V
+ * (ekv_rope_append), and attend a batch whose sequences share prefixes
+ * (ekv_attn_decode_shared).  All three can be captured in a HIP graph and
+ * replayed.  (ekv_rope_freqs makes the rotary table, once, on the host.)
+ */
+
+/*
+ * Free physical blocks, as a ring: block number k of the count free ones is
+ * ids[(head + k) % capacity].  The cursor is {head, count}; a call reads
+ * `cursor` and writes `cursor_out`, which may be the same array (the list is
+ * then consumed in place) or another one (the call can be made again from
+ * the same state).  Blocks are given out from the head, first in first out;
+ * the caller appends returned ones (a demotion's freed list, a finished
+ * sequence's blocks) behind the last and raises the count, ordered with the
+ * calls on the stream.  A head outside the ring is taken modulo the capacity
+ * and a count outside [0, capacity] clamped into it.
+ */
+typedef struct {
+  const int32_t* ids;      /* device int32 [capacity] */
+  const int32_t* cursor;   /* device int32 [2] */
+  int32_t* cursor_out;     /* device int32 [2] */
+  int32_t capacity;
+  int32_t num_blocks;      /* of the pool that the ids name */
+} ekv_free_list;
+
+/* Why ekv_extend took nothing (bits of status[0]). */
+enum {
+  EKV_EXTEND_ROW = 1,      /* a length or a number of new tokens is negative, or the sum exceeds max_blocks*page_size */
+  EKV_EXTEND_TOKENS = 2,   /* more new tokens than max_tokens */
+  EKV_EXTEND_BLOCKS = 4,   /* more new blocks than free ones */
+  EKV_EXTEND_BASE = 8      /* new tokens would go into a partly filled block tagged BASE */
+};
+
+/*
+ * Block tables and slot maps from request lengths (page size 16).  Sequence
+ * s holds seq_lens[s] tokens and gets new_lens[s] more (NULL: one each).  In
+ * order of the sequences, every block that the new tokens need beyond those
+ * in use takes the next free block: its table entry is written and its tag
+ * set to TARGET.  For token i of sequence s, at row r = cu_q[s] + i:
+ *   p            = seq_lens[s] + i, its position in the cache
+ *   slots[r]     = block_table[s][p / 16] * 16 + p % 16 (ekv_append_kv,
+ *                  ekv_rope_append); -1 if that block is outside the pool
+ *   positions[r] = p + start[s], its position in the request (start: the
+ *                  length of a shared prefix in front of it, say; NULL: 0)
+ * cu_q [batch + 1] are the exclusive sums of new_lens (ekv_attn_prefill), and
+ * seq_lens_out[s] = seq_lens[s] + new_lens[s]; seq_lens_out may be seq_lens.
+ * Rows from cu_q[batch] to max_tokens get slot -1 and position 0, so that
+ * later calls may run over max_tokens rows whatever the number of tokens.
+ * The call takes all or nothing: if something does not fit, table, tags,
+ * lengths and free list stay as they are (seq_lens_out = seq_lens, cursor_out
+ * = cursor with the clamping above), cu_q is all zero and every slot -1.
+ *   block_table device int32 [batch][max_blocks], tags device uint8 of the
+ *               same shape or NULL; entries of blocks in use are read only
+ *   status      device int32 [4]: {reasons (EKV_EXTEND_*, 0 = done), new
+ *               tokens, new blocks, blocks left free}; the sums count the
+ *               sequences that are valid, and saturate at 2^30
+ * tags, new_lens, start and positions may be NULL.  The arrays written must
+ * not overlap each other or those read, but for the two pairs named above.
+ * batch <= 4096.
+ * Errors: EKV_ERR_INVALID (NULL pointers, sizes), EKV_ERR_UNSUPPORTED (batch,
+ * or slots that need more than 31 bits), EKV_ERR_HIP.
+ */
+ekv_status ekv_extend(const ekv_free_list* free_list, int32_t batch, int32_t max_blocks, const int32_t* seq_lens,
+                      const int32_t* new_lens, const int32_t* start, int32_t* block_table, uint8_t* tags,
+                      int32_t* seq_lens_out, int32_t* cu_q, int32_t max_tokens, int32_t* slots, int32_t* positions,
+                      int32_t* status, hipStream_t stream);
+
+/* Pair i of a head's rotated part: elements (i, i + rotary_dim / 2), or (2i, 2i + 1). */
+enum { EKV_ROPE_HALF = 0, EKV_ROPE_PAIRS = 1 };
+
+/*
+ * Angles a position, theta_i = base^(-2i / rotary_dim), and for contexts
+ * `factor` times longer:
+ *   PLAIN   theta_i
+ *   LINEAR  theta_i / factor
+ *   BASE    theta_i of the base  base * factor^(rotary_dim / (rotary_dim - 2))
+ *   PARTS   theta_i (g + (1 - g) / factor), g = (context theta_i / (2 pi) - low)
+ *           / (high - low) clamped to [0, 1]: pairs that make at most `low` turns
+ *           over the trained context are stretched whole, from `high` on not at all
+ */
+enum { EKV_ROPE_PLAIN = 0, EKV_ROPE_LINEAR = 1, EKV_ROPE_BASE = 2, EKV_ROPE_PARTS = 3 };
+
+typedef struct {
+  const uint64_t* turns;   /* device uint64 [rotary_dim / 2]: theta_i / (2 pi) in units of 2^-64 turns (ekv_rope_freqs) */
+  int32_t rotary_dim;      /* elements of a head that turn, from its first: a multiple of 16, at most head_dim */
+  int32_t layout;          /* EKV_ROPE_HALF or EKV_ROPE_PAIRS */
+  float magnitude;         /* multiplies the turned elements (1: a plain rotation) */
+} ekv_rope;
+
+/*
+ * The rotary table of one of the rules above, host only: writes
+ * h_turns_out [rotary_dim / 2], to be copied to the device once.  Fixed point
+ * keeps any 32-bit position exact: full turns fall off a 64-bit product.
+ * factor is not used by PLAIN, context, low and high only by PARTS.
+ * Errors: EKV_ERR_INVALID (NULL pointer, base or factor below 1, unknown rule,
+ * PARTS without a context or with low >= high), EKV_ERR_UNSUPPORTED.
+ */
+ekv_status ekv_rope_freqs(int32_t rotary_dim, double base, int32_t scaling, double factor, double context, double low,
+                          double high, uint64_t* h_turns_out);
+
+/*
+ * Rotary positions fused with the append.  For row r < n, at position
+ * t = positions[r], every query and key head turns: pair i of its rotated part
+ * becomes
+ *   x' = magnitude (x cos(t theta_i) - y sin(t theta_i))
+ *   y' = magnitude (y cos(t theta_i) + x sin(t theta_i))
+ * in 32 bits and is rounded once; the rest of the head passes through.  The
+ * turned query goes to q_out, the turned key and the value to token slot
+ * slots[r] of the pool, as TARGET (for an 8-bit pool both are rounded to the
+ * nearest E5M2 value).  Rows whose slot is outside the pool (-1, as
+ * ekv_extend leaves them) write no K and V; their query is turned as well.
+ *   positions, slots  device int32 [n]; slots inside the pool must be distinct
+ *                     and lie in TARGET blocks
+ *   q, q_out          rows of num_q_heads * head_dim values, k, v of
+ *                     num_kv_heads * head_dim, of the query dtype (the pool's, or
+ *                     FP16 for an 8-bit pool); row r starts at r * stride
+ *                     values, so q, k and v may be parts of one projection's
+ *                     rows.  Strides are multiples of 8, rows 16-byte aligned.
+ *                     q_out may be q (with the same stride); the rows written
+ *                     must not overlap the rest of the inputs otherwise.
+ * Errors: EKV_ERR_INVALID, EKV_ERR_UNSUPPORTED, EKV_ERR_HIP.
+ */
+ekv_status ekv_rope_append(const ekv_pool* pool, const ekv_rope* rope, int32_t n, const int32_t* positions,
+                           const int32_t* slots, const void* q, int64_t q_stride, int32_t num_q_heads, const void* k,
+                           int64_t k_stride, const void* v, int64_t v_stride, void* q_out, int64_t q_out_stride,
+                           hipStream_t stream);
+
+/*
+ * Decode attention over shared prefixes, one query token per sequence.
+ * `prefixes` describes the prefixes as `batch` does the sequences: a row of
+ * its table, tags and lengths per prefix, its own mode, the same
+ * num_q_heads; both name blocks of the one pool.  Sequences
+ * group_start[p] .. group_start[p+1] - 1 stand behind prefix p; sequences
+ * before group_start[0] or from group_start[prefixes->batch] on behind none.
+ * Query head h of sequence s (KV head h / G, G = num_q_heads / num_kv_heads)
+ * gives
+ *   out[s][h] = softmax(scale * q[s][h] . [K_p; K_s]^T) [V_p; V_s]
+ * over the prefix's lens[p] tokens and the sequence's own seq_lens[s], each
+ * block read in its mode (as ekv_attn_decode).  A prefix's K and V are read
+ * for all of its sequences at once, not once for each.  seq_lens counts
+ * the sequence's own tokens only; either part may be empty, and a sequence
+ * with no token at all yields zeros.
+ *   group_start  device int32 [prefixes->batch + 1], nondecreasing, inside
+ *                [0, batch->batch] (clamped and made so); may be NULL when
+ *                prefixes->batch is 0
+ *   q, out       device [batch][num_q_heads][head_dim], out_dtype = the query
+ *                dtype or EKV_DTYPE_FP32
+ *   ws           device scratch of ekv_decode_shared_workspace_bytes() bytes,
+ *                16-byte aligned; needs no preparation and keeps nothing between
+ *                calls; calls that share one must be ordered
+ * ws, q, out and the pool are 16-byte aligned.
+ * Transitions of a prefix's pairs are made on its row like any sequence's
+ * (ekv_demote on the prefixes' table), while no attention call reads it.
+ * Errors: as ekv_attn_decode.
+ */
+size_t ekv_decode_shared_workspace_bytes(const ekv_pool* pool, const ekv_batch* prefixes, const ekv_batch* batch);
+ekv_status ekv_attn_decode_shared(const ekv_pool* pool, const ekv_batch* prefixes, const int32_t* group_start,
+                                  const ekv_batch* batch, const void* q, void* out, int32_t out_dtype, float scale,
+                                  void* ws, size_t ws_bytes, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -30,6 +30,9 @@ What it computes, and where the paper defines it:
 * ``fp8``        -- the 8-bit TARGET (E5M2) / 4-bit BASE instance of the
   same contract: encoding, packed nibble pairs, transitions, decode and
   prefill (App. C.5, last paragraph).
+* ``serve``      -- the serving step around the cache: table extension from
+  request lengths, rotary positions, decode over shared prefixes (§2.1, §3.4:
+  the paged engine that the runtime sits in).
 
 Readings of points the paper leaves open (pair membership, which block of a
 pair survives demotion, the byte layout inside a packed block, where the
@@ -41,4 +44,4 @@ formula (closed forms, exhaustive enumeration, brute force on tiny inputs,
 library routines, invariants); see the ``tests/test_oracle_*.py`` files.
 """
 
-from . import encoding, paged, attention, transitions, lowering, validate, control, fp8  # noqa: F401
+from . import encoding, paged, attention, transitions, lowering, validate, control, fp8, serve  # noqa: F401

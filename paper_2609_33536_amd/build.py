@@ -18,7 +18,8 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libekv.so")
 TIMELINE_LIB = os.path.join(HERE, "libekv_timeline.so")
-SOURCES = ["api.hip", "control.hip", "decode.hip", "prefill.hip", "transition.hip", "validate.hip"]
+SOURCES = ["api.hip", "api_serve.hip", "control.hip", "decode.hip", "extend.hip", "prefill.hip", "rope.hip", "shared.hip",
+           "transition.hip", "validate.hip"]
 ARCH = "gfx950"
 
 FLAGS = [

@@ -1,0 +1,169 @@
+// Rotary positions of queries and keys, with the rotated keys and the values
+// written to their cache slots.
+//
+// Pair i of a head (elements x, y) at position t turns by the angle t theta_i:
+//   x' = r (x cos - y sin), y' = r (y cos + x sin),  r the caller's magnitude.
+// Angles of far positions need more than a float's 24 bits (at t = 10^6 a float
+// product is off by up to 0.03 rad), so theta_i comes as a fixed-point fraction of a
+// turn, T_i = theta_i / (2 pi) 2^64: t T_i mod 2^64 is the exact phase of T_i's
+// multiple, its top 32 bits keep 2^-32 of a turn, and full turns fall away without
+// a division.
+//
+// 8 lanes hold a head's 128 elements, lane c the pairs 8c .. 8c + 7 (half layout:
+// elements 8c.. and rotary_dim / 2 + 8c..; pair layout: 16c .. 16c + 15), so that a
+// lane's cosines and sines serve every head that its wave turns.
+#include "common.h"
+#include "rope.h"
+
+namespace ekv {
+namespace {
+
+constexpr int kWaves = 4;
+
+// cos and sin of 2 pi p 2^-32: the nearest quarter turn taken off exactly, then the
+// Taylor polynomials on [-pi/4, pi/4] (to x^10 and x^9: truncated below 2e-9).
+__device__ __forceinline__ void cos_sin(uint32_t p, float& c, float& s) {
+  const uint32_t quarter = (p + 0x20000000u) >> 30;
+  const int32_t rest = (int32_t)(p - (quarter << 30));
+  const float x = (float)rest * 1.46291807926715968e-9f;   // 2 pi / 2^32
+  const float z = x * x;
+  const float sn = x + x * z * (-1.0f / 6 + z * (1.0f / 120 + z * (-1.0f / 5040 + z * (1.0f / 362880))));
+  const float cs = 1.0f + z * (-0.5f + z * (1.0f / 24 + z * (-1.0f / 720 + z * (1.0f / 40320 + z * (-1.0f / 3628800)))));
+  const bool swap = quarter & 1;
+  c = swap ? sn : cs;
+  s = swap ? cs : sn;
+  if ((quarter + 1) & 2) c = -c;
+  if (quarter & 2) s = -s;
+}
+
+// 8 floats -> 8 words of T (to nearest) or, for an 8-bit pool, 8 E5M2 bytes (to nearest, straight from 32 bits)
+template <typename T>
+__device__ __forceinline__ u32x4 words8(const float (&x)[8]) {
+  u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float back;
+    w[i] = (uint32_t)Mma<T>::round(x[2 * i], &back) | ((uint32_t)Mma<T>::round(x[2 * i + 1], &back) << 16);
+  }
+  return w;
+}
+__device__ __forceinline__ u32x2 bytes8(const float (&x)[8]) {
+  u32x2 w;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    int d = __builtin_amdgcn_cvt_pk_bf8_f32(x[4 * i], x[4 * i + 1], 0, false);
+    w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_bf8_f32(x[4 * i + 2], x[4 * i + 3], d, true);
+  }
+  return w;
+}
+template <typename T>
+__device__ __forceinline__ void floats8(u32x4 w, float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = Mma<T>::widen((uint16_t)w[i]);
+    x[2 * i + 1] = Mma<T>::widen((uint16_t)(w[i] >> 16));
+  }
+}
+
+template <typename T, bool F8>
+__global__ __launch_bounds__(64 * kWaves) void rope_kernel(RopeArgs a) {
+  const int lane = threadIdx.x & 63, c = lane & 7;
+  const int rows = a.num_q_heads + 2 * a.num_kv_heads;   // rows of a token: query heads, key heads, value heads
+  const int parts = (rows + a.rows_per_wave - 1) / a.rows_per_wave;
+  const int64_t item = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+  if (item >= (int64_t)a.n * parts) return;
+  const int token = (int)(item / parts), part = (int)(item % parts);
+  const int row_end = min(rows, (part + 1) * a.rows_per_wave);
+
+  const int slot = a.slots[token];
+  const int64_t position = a.positions[token];
+  const bool in_pool = slot >= 0 && slot / kPage < a.num_blocks;   // (outside the pool: the cache is left as it is)
+  const int turned = a.rotary_dim / 16;                            // lanes whose pairs turn
+  float cs[8], sn[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    cs[i] = 1.0f;
+    sn[i] = 0.0f;
+    if (c < turned) {
+      const uint64_t phase = (uint64_t)position * a.turns[8 * c + i];
+      cos_sin((uint32_t)((phase + 0x80000000ull) >> 32), cs[i], sn[i]);
+      cs[i] *= a.magnitude;
+      sn[i] *= a.magnitude;
+    }
+  }
+  // this lane's two 8-element chunks of a head
+  const int chunk0 = a.pairs ? 2 * c : (c < turned ? c : 2 * turned + 2 * (c - turned));
+  const int chunk1 = a.pairs ? 2 * c + 1 : (c < turned ? turned + c : chunk0 + 1);
+
+  for (int r = part * a.rows_per_wave + (lane >> 3); r < row_end; r += 8) {
+    const int head = r < a.num_q_heads ? r : (r - a.num_q_heads) % a.num_kv_heads;
+    const int kind = r < a.num_q_heads ? 0 : (r < a.num_q_heads + a.num_kv_heads ? 1 : 2);   // query, key, value
+    if (kind != 0 && !in_pool) continue;
+    const uint16_t* src = (kind == 0 ? a.q + token * a.q_stride : (kind == 1 ? a.k + token * a.k_stride : a.v + token * a.v_stride)) +
+                          (size_t)head * kHeadDim;
+    u32x4 w0 = *reinterpret_cast<const u32x4*>(src + 8 * chunk0), w1 = *reinterpret_cast<const u32x4*>(src + 8 * chunk1);
+    float x[8], y[8];
+    if (kind != 2 && c < turned) {
+      floats8<T>(w0, x);
+      floats8<T>(w1, y);
+      if (a.pairs) {   // elements 16 c + 2 i, + 1
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float x0 = x[2 * i], x1 = x[2 * i + 1], y0 = y[2 * i], y1 = y[2 * i + 1];
+          x[2 * i] = x0 * cs[i] - x1 * sn[i];
+          x[2 * i + 1] = x1 * cs[i] + x0 * sn[i];
+          y[2 * i] = y0 * cs[4 + i] - y1 * sn[4 + i];
+          y[2 * i + 1] = y1 * cs[4 + i] + y0 * sn[4 + i];
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float x0 = x[i], y0 = y[i];
+          x[i] = x0 * cs[i] - y0 * sn[i];
+          y[i] = y0 * cs[i] + x0 * sn[i];
+        }
+      }
+      w0 = words8<T>(x);
+      w1 = words8<T>(y);
+    } else if (F8) {
+      floats8<T>(w0, x);
+      floats8<T>(w1, y);
+    }
+    if (kind == 0) {
+      uint16_t* dst = a.q_out + token * a.out_stride + (size_t)head * kHeadDim;
+      *reinterpret_cast<u32x4*>(dst + 8 * chunk0) = w0;
+      *reinterpret_cast<u32x4*>(dst + 8 * chunk1) = w1;
+    } else {
+      const size_t at = (((size_t)(slot / kPage) * 2 + (kind - 1)) * a.num_kv_heads + head) * kTileWords + (slot % kPage) * kHeadDim;
+      if constexpr (F8) {
+        uint8_t* dst = static_cast<uint8_t*>(a.pool) + at;
+        *reinterpret_cast<u32x2*>(dst + 8 * chunk0) = bytes8(x);
+        *reinterpret_cast<u32x2*>(dst + 8 * chunk1) = bytes8(y);
+      } else {
+        uint16_t* dst = static_cast<uint16_t*>(a.pool) + at;
+        *reinterpret_cast<u32x4*>(dst + 8 * chunk0) = w0;
+        *reinterpret_cast<u32x4*>(dst + 8 * chunk1) = w1;
+      }
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_rope(const RopeArgs& a, int dtype, hipStream_t st) {
+  if (a.n == 0) return hipSuccess;
+  RopeArgs b = a;
+  const int rows = a.num_q_heads + 2 * a.num_kv_heads;
+  b.rows_per_wave = a.n >= 2048 ? rows : 8;
+  const int64_t items = (int64_t)a.n * ((rows + b.rows_per_wave - 1) / b.rows_per_wave);
+  const dim3 grid((unsigned)((items + kWaves - 1) / kWaves)), block(64 * kWaves);
+  switch (dtype) {
+    case 0: hipLaunchKernelGGL((rope_kernel<Bf16, false>), grid, block, 0, st, b); break;
+    case 1: hipLaunchKernelGGL((rope_kernel<Fp16, false>), grid, block, 0, st, b); break;
+    case 3: hipLaunchKernelGGL((rope_kernel<Fp16, true>), grid, block, 0, st, b); break;
+    default: return hipErrorInvalidValue;
+  }
+  return hipGetLastError();
+}
+
+}  // namespace ekv

@@ -41,6 +41,16 @@ class Batch(ctypes.Structure):
                 ("boundaries", ctypes.c_void_p)]
 
 
+class FreeList(ctypes.Structure):
+    _fields_ = [("ids", ctypes.c_void_p), ("cursor", ctypes.c_void_p), ("cursor_out", ctypes.c_void_p),
+                ("capacity", ctypes.c_int32), ("num_blocks", ctypes.c_int32)]
+
+
+class Rope(ctypes.Structure):
+    _fields_ = [("turns", ctypes.c_void_p), ("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32),
+                ("magnitude", ctypes.c_float)]
+
+
 class CtrlConfig(ctypes.Structure):
     _fields_ = [("min_batch", ctypes.c_int32), ("decay", ctypes.c_int32), ("a_max", ctypes.c_int32),
                 ("sink_pairs", ctypes.c_int32), ("recent_pairs", ctypes.c_int32), ("policy", ctypes.c_int32),
@@ -61,8 +71,14 @@ NO_INDEX = 0x7FFFFFFF
 CTRL_EAGER_PROMOTION, CTRL_NO_PROMOTION = 1, 2
 
 
+# reasons of ekv_extend (bits of its status[0])
+EXTEND_ROW, EXTEND_TOKENS, EXTEND_BLOCKS, EXTEND_BASE = 1, 2, 4, 8
+ROPE_LAYOUTS = {"half": 0, "pairs": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "parts": 3}
+
 # name -> (restype, argtypes), in the order of include/ekv.h
 _P, _I, _U, _F, _S = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t, ctypes.c_float, ctypes.c_void_p
+_L, _D = ctypes.c_int64, ctypes.c_double
 SIGNATURES = {
     "ekv_status_string": (ctypes.c_char_p, [_I]),
     "ekv_last_error": (ctypes.c_char_p, []),
@@ -91,6 +107,13 @@ SIGNATURES = {
                                _I, _I, _I, _P, _I, _P]),
     "ekv_ctrl_promotion": (_I, [ctypes.POINTER(CtrlConfig), ctypes.POINTER(CtrlState), _I, _I, _P, _P, _I,
                                 _I, _I, _P, _I, _P]),
+    "ekv_extend": (_I, [ctypes.POINTER(FreeList), _I, _I, _P, _P, _P, _P, _P, _P, _P, _I, _P, _P, _P, _S]),
+    "ekv_rope_freqs": (_I, [_I, _D, _I, _D, _D, _D, _D, _P]),
+    "ekv_rope_append": (_I, [ctypes.POINTER(Pool), ctypes.POINTER(Rope), _I, _P, _P, _P, _L, _I, _P, _L, _P, _L, _P,
+                             _L, _S]),
+    "ekv_decode_shared_workspace_bytes": (_U, [ctypes.POINTER(Pool), ctypes.POINTER(Batch), ctypes.POINTER(Batch)]),
+    "ekv_attn_decode_shared": (_I, [ctypes.POINTER(Pool), ctypes.POINTER(Batch), _P, ctypes.POINTER(Batch), _P, _P, _I,
+                                    _F, _P, _U, _S]),
 }
 
 _lib = None
@@ -403,3 +426,110 @@ def ctrl_promotion(cfg, state, free_post, slack, tags, seq_lens, page=PAGE):
                                     bsz, max_blocks, page, out.ctypes.data_as(ctypes.c_void_p), cap,
                                     ctypes.byref(n)))
     return out[:n.value].copy()
+
+
+def _typed(t, dtype, shape, name):
+    """Device pointer of a contiguous tensor of this dtype and shape (None
+    passes): the kernels take sizes from the call, so a tensor of another
+    size would be read or written past its end."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise EkvError(ERR_INVALID, f"{name} must be {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    return _ptr(t)
+
+
+def make_free_list(ids, cursor, num_blocks, cursor_out=None):
+    """Describe a ring of free blocks: ids int32 [capacity], cursor int32 [2]
+    = {head, count}; cursor_out defaults to cursor (consumed in place)."""
+    import torch
+    cursor_out = cursor if cursor_out is None else cursor_out
+    f = FreeList(_typed(ids, torch.int32, (ids.numel(),), "ids"), _typed(cursor, torch.int32, (2,), "cursor"),
+                 _typed(cursor_out, torch.int32, (2,), "cursor_out"), ids.numel(), num_blocks)
+    f.tensors = (ids, cursor, cursor_out)   # (kept: the struct holds their addresses)
+    return f
+
+
+def extend(free_list, seq_lens, new_lens, block_table, tags, seq_lens_out, cu_q, slots, positions, status, start=None,
+           stream=None):
+    """ekv_extend: cache room for new_lens[s] (None: one) more tokens of every
+    sequence.  slots (and positions) hold one row per token and set the most
+    tokens of the call; seq_lens_out may be seq_lens."""
+    import torch
+    bsz, max_blocks = block_table.shape
+    i32, rows = torch.int32, slots.numel()
+    if rows >= 1 << 30:   # (before the C call's 32-bit argument cuts it off)
+        raise EkvError(ERR_UNSUPPORTED, "at most 2^30 - 1 token rows")
+    _check(lib().ekv_extend(ctypes.byref(free_list), bsz, max_blocks, _typed(seq_lens, i32, (bsz,), "seq_lens"),
+                            _typed(new_lens, i32, (bsz,), "new_lens"), _typed(start, i32, (bsz,), "start"),
+                            _typed(block_table, i32, (bsz, max_blocks), "block_table"),
+                            _typed(tags, torch.uint8, (bsz, max_blocks), "tags"),
+                            _typed(seq_lens_out, i32, (bsz,), "seq_lens_out"), _typed(cu_q, i32, (bsz + 1,), "cu_q"),
+                            rows, _typed(slots, i32, (rows,), "slots"), _typed(positions, i32, (rows,), "positions"),
+                            _typed(status, i32, (4,), "status"), _stream(stream)))
+
+
+def rope_freqs(rotary_dim, base=10000.0, scaling="none", factor=1.0, context=0.0, low=1.0, high=4.0):
+    """ekv_rope_freqs: the rotary table uint64 [rotary_dim / 2] (host); copy it
+    to the device once, as int64, for :func:`make_rope`."""
+    out = np.zeros(max(int(rotary_dim) // 2, 0), dtype=np.uint64)
+    if scaling not in ROPE_SCALINGS:
+        raise EkvError(ERR_INVALID, f"unknown scaling {scaling!r}")
+    _check(lib().ekv_rope_freqs(int(rotary_dim), base, ROPE_SCALINGS[scaling], factor, context, low, high,
+                                out.ctypes.data_as(ctypes.c_void_p)))
+    return out
+
+
+def make_rope(turns, rotary_dim, layout="half", magnitude=1.0):
+    """Describe a rotation: turns is the table of :func:`rope_freqs` as a
+    device int64 tensor."""
+    import torch
+    if layout not in ROPE_LAYOUTS:
+        raise EkvError(ERR_INVALID, f"unknown layout {layout!r}")
+    r = Rope(_typed(turns, torch.int64, (rotary_dim // 2,), "turns"), rotary_dim, ROPE_LAYOUTS[layout], magnitude)
+    r.tensors = (turns,)   # (kept: the struct holds its address)
+    return r
+
+
+def _rows(t, shape, dtype, name):
+    """(pointer, row stride) of a tensor [n][heads][128] whose heads are packed."""
+    if t.dtype != dtype or tuple(t.shape) != shape:
+        raise EkvError(ERR_INVALID, f"{name} must be {dtype} {shape}, got {t.dtype} {tuple(t.shape)}")
+    if not t.is_cuda:
+        raise EkvError(ERR_INVALID, "device argument must be a GPU tensor")
+    if t.stride(2) != 1 or t.stride(1) != HEAD_DIM:
+        raise EkvError(ERR_INVALID, f"the heads of a row of {name} must be packed")
+    # (a single row's stride says nothing)
+    return t.data_ptr(), t.stride(0) if shape[0] > 1 else max(t.stride(0), shape[1] * HEAD_DIM)
+
+
+def rope_append(pool, rope, positions, slots, q, k, v, q_out, stream=None):
+    """ekv_rope_append: q, q_out [n][Hq][128] and k, v [n][Hkv][128] may be
+    views of wider rows (the heads of a row packed)."""
+    import torch
+    n, hq, hkv = q.shape[0], q.shape[1], pool.num_kv_heads
+    dtype = torch.bfloat16 if pool.dtype == DTYPE_BF16 else torch.float16
+    (qp, qs), (op, os_) = _rows(q, (n, hq, HEAD_DIM), dtype, "q"), _rows(q_out, (n, hq, HEAD_DIM), dtype, "q_out")
+    (kp, ks), (vp, vs) = _rows(k, (n, hkv, HEAD_DIM), dtype, "k"), _rows(v, (n, hkv, HEAD_DIM), dtype, "v")
+    _check(lib().ekv_rope_append(ctypes.byref(pool), ctypes.byref(rope), n, _typed(positions, torch.int32, (n,), "positions"),
+                                 _typed(slots, torch.int32, (n,), "slots"), qp, qs, hq, kp, ks, vp, vs, op, os_,
+                                 _stream(stream)))
+
+
+def decode_shared_workspace_bytes(pool, prefixes, batch):
+    return lib().ekv_decode_shared_workspace_bytes(ctypes.byref(pool), ctypes.byref(prefixes), ctypes.byref(batch))
+
+
+def decode_shared_workspace(pool, prefixes, batch, device="cuda"):
+    """Scratch for :func:`attn_decode_shared` (it needs no preparation)."""
+    import torch
+    return torch.empty(decode_shared_workspace_bytes(pool, prefixes, batch), dtype=torch.uint8, device=device)
+
+
+def attn_decode_shared(pool, prefixes, group_start, batch, q, out, scale, ws, stream=None):
+    """Decode of sequences behind shared prefixes: `prefixes` is a
+    :func:`make_batch` of the prefixes' rows, group_start int32
+    [prefixes.batch + 1] the first sequence behind each."""
+    _check(lib().ekv_attn_decode_shared(ctypes.byref(pool), ctypes.byref(prefixes), _ptr(group_start),
+                                        ctypes.byref(batch), _ptr(q), _ptr(out), dtype_code(out.dtype), scale, _ptr(ws),
+                                        ws.numel() * ws.element_size(), _stream(stream)))

@@ -15,6 +15,7 @@ new blocks from the head.
 through :mod:`ekv`.
 """
 
+import contextlib
 from collections import deque
 
 import numpy as np
@@ -98,6 +99,28 @@ class HostMirror:
         new = self.reserve_refine(pairs)
         self.publish_refine(pairs, new)
         return new
+
+    def plan_extend(self, new_lens):
+        """Give every sequence cache room for new_lens[s] more tokens: blocks
+        from the head of the free pool, sequence by sequence, as TARGET.
+        Returns the blocks taken, in order; nothing changes if they do not
+        fit."""
+        new_lens = np.asarray(new_lens, dtype=np.int32)
+        total = self.seq_lens.astype(np.int64) + new_lens
+        if new_lens.shape != self.seq_lens.shape or (new_lens < 0).any() or (total > self.bt.shape[1] * self.page).any():
+            raise ekv.EkvError(ekv.ERR_INVALID, "new lengths do not fit the sequences' table rows")
+        old = -(-self.seq_lens // self.page)
+        need = -(-total // self.page) - old
+        n = int(need.sum())
+        if n > len(self.free):
+            raise ekv.EkvError(ekv.ERR_INVALID, f"{n} blocks needed, {len(self.free)} free")
+        taken = np.array([self.free.popleft() for _ in range(n)], dtype=np.int32)
+        s = np.repeat(np.arange(len(need)), need)
+        i = old[s] + np.arange(n) - np.repeat(np.cumsum(need) - need, need)
+        self.bt[s, i] = taken
+        self.tags[s, i] = 0
+        self.seq_lens = total.astype(np.int32)
+        return taken
 
     def lower(self):
         return ekv.lower(self.tags, self.seq_lens, self.page)
@@ -190,6 +213,26 @@ class PagedKV:
 
     def append(self, slots, k, v, stream=None):
         ekv.append_kv(self.pool, slots, k, v, stream)
+
+    def extend(self, new_lens, start=None, stream=None):
+        """Cache room for new_lens[s] more tokens of every sequence: table, tags
+        and lengths grow in the mirror and, by one launch, on the device.
+        Returns (cu_q, slots, positions) on the device, a row per new token;
+        positions count from start[s] (device int32, default 0)."""
+        import torch
+        with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+            new_lens = np.asarray(new_lens, dtype=np.int32)
+            taken = self.mirror.plan_extend(new_lens)
+            rows = int(new_lens.sum())
+            # one upload: the new lengths, the blocks taken, and the cursor over them
+            up = self._upload(np.concatenate([new_lens, taken, np.array([0, 0, len(taken)], dtype=np.int32)]))
+            b = len(new_lens)
+            free = ekv.make_free_list(up[b:b + len(taken) + 1], up[-2:], self.mirror.num_blocks)
+            out = torch.empty(b + 1 + 2 * rows + 4, dtype=torch.int32, device=self.device)
+            cu_q, slots, positions = out[:b + 1], out[b + 1:b + 1 + rows], out[b + 1 + rows:b + 1 + 2 * rows]
+            ekv.extend(free, self.seq_lens, up[:b], self.bt, self.tags, self.seq_lens, cu_q, slots, positions, out[-4:],
+                       start, stream)
+        return cu_q, slots, positions
 
 
 class AsyncPromotion:

@@ -20,7 +20,7 @@ bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0;
 
 // ---- shared-prefix decode -------------------------------------------------
 
-// Scratch of a call: [plan | (m, l) and o of 32-column slots | of G-column slots],
+// Scratch of a call: [12 ints a sequence for the merge | (m, l) and o of 32-column slots | of G-column slots],
 // 256-B aligned parts.  Slots: at most one per 32 columns (or part of 32) of a group
 // and KV head, and 4 per workgroup for the segments that workers cut; likewise one
 // per sequence and KV head.
@@ -38,13 +38,13 @@ ekv_status plan_shared(const ekv_pool* p, const ekv_batch* prefixes, const ekv_b
   const int64_t work_t = hkv * tiles * units_p, work_s = hkv * rows * units_s;
   if (work_t >= (1 << 30) || work_s >= (1 << 30) || columns * hkv >= (1 << 30) || prefixes->batch >= (1 << 24))
     return fail(EKV_ERR_UNSUPPORTED, "batch too large for one shared-prefix decode call");
-  l->min_units = (int)std::max<int64_t>(1, std::min<int64_t>(4, units_p / 16));
-  const int64_t wanted = (work_t + hkv * groups * units_p / 4 + work_s / 4) / l->min_units + 3;
+  l->min_units = (int)std::max<int64_t>(1, std::min<int64_t>(4, units_p / 16));   // (of the prefixes: pieces to merge)
+  const int64_t wanted = (work_t + hkv * groups * units_p / 4 + work_s / 4) / l->min_units + 4;
   l->grid = (int)std::min<int64_t>(kMaxSharedGrid, wanted);
-  l->wide_slots = hkv * (columns / 32 + groups) + 4 * l->grid;
+  l->wide_slots = hkv * (columns / 32 + groups) + columns / 32 + 4 * groups + 4 * l->grid;
   l->own_slots = hkv * rows + 4 * l->grid;
   auto align = [](size_t x) { return (x + 255) & ~(size_t)255; };
-  l->ml_wide = align(sizeof(int32_t) * (4 + 8 * (size_t)prefixes->batch + 2 * (size_t)rows));
+  l->ml_wide = align(12 * sizeof(int32_t) * (size_t)rows);
   l->o_wide = align(l->ml_wide + (size_t)l->wide_slots * 32 * 8);
   l->ml_own = align(l->o_wide + (size_t)l->wide_slots * 32 * kHeadDim * 4);
   l->o_own = align(l->ml_own + (size_t)l->own_slots * group * 8);
@@ -253,7 +253,7 @@ ekv_status ekv_attn_decode_shared(const ekv_pool* pool, const ekv_batch* prefixe
     a.num_q_heads = batch->num_q_heads;
     a.log2_group = __builtin_ctz((unsigned)group);
     a.out_fp32 = out_dtype == EKV_DTYPE_FP32;
-    a.grid = std::max(3, std::min(l.grid, resident));
+    a.grid = std::max(4, std::min(l.grid, resident));
     a.min_units = l.min_units;
     a.scale_log2 = log2e_scale(scale);
     const bool elastic = (prefixes->batch > 0 && prefixes->mode != EKV_MODE_NATIVE) || batch->mode != EKV_MODE_NATIVE;

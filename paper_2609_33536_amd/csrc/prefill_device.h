@@ -172,6 +172,47 @@ struct Stager {
       dma16(src2 + v_off, off, to + kPlanePf + kGroup);
     }
   }
+  // The two planes of a quarter to places of their own (K first: kLoads / 2 loads each).
+  __device__ __forceinline__ void load_planes(uint64_t tile, bool base, int q, uint32_t k_slot, uint32_t v_slot) const {
+    const uint32_t at = quarter_offset(q);
+    const uint64_t packed = tile + (uint32_t)(q >> 1) * (kTileP / 2);
+    if constexpr (F8) {
+      const uint32_t off = base ? src_n : src_b;
+      const uint64_t src = base ? packed + (q & 1) * 8 * (kHeadDim / 2) : tile + (q & 1) * 8 * kHeadDim;
+      dma16(src, off, k_slot + at);
+      dma16(src + v_off, off, v_slot + at);
+    } else {
+      const uint32_t off = base ? src_b : src_t;
+      const uint64_t src = base ? packed + (q & 1) * 8 * kHeadDim : tile + (q & 1) * 8 * 2 * kHeadDim;
+      const uint64_t src2 = src + (base ? 0 : 1024);
+      dma16(src, off, k_slot + at);
+      dma16(src2, off, k_slot + at + kGroup);
+      dma16(src + v_off, off, v_slot + at);
+      dma16(src2 + v_off, off, v_slot + at + kGroup);
+    }
+  }
+  // As widen, for one plane's slot.
+  __device__ __forceinline__ void widen_plane(char* slot, bool base, int q, int lane) const {
+    if (!F8 && !base) return;
+    char* at = slot + quarter_offset(q);
+    u32x4 raw;
+    if (F8 && base) {
+      const u32x2 x = *reinterpret_cast<const u32x2*>(at + raw_n);
+      const u32x2 lo = widen_nibbles(x.x), hi = widen_nibbles(x.y);
+      raw = u32x4{lo.x, lo.y, hi.x, hi.y};
+    } else {
+      raw = *reinterpret_cast<const u32x4*>(at + 16 * lane);
+    }
+    *reinterpret_cast<u32x4*>(at + dst) = expand_base8(raw.xy);
+    *reinterpret_cast<u32x4*>(at + dst + 16) = expand_base8(raw.zw);
+  }
+  __device__ __forceinline__ void clear_tail(char* v_slot, int q, int key0, int valid) const {
+    if (key0 + 2 * kPage > valid && key0 + 8 * q + row >= valid) {
+      char* at = v_slot + quarter_offset(q) + dst;
+      *reinterpret_cast<u32x4*>(at) = u32x4{0u, 0u, 0u, 0u};
+      *reinterpret_cast<u32x4*>(at + 16) = u32x4{0u, 0u, 0u, 0u};
+    }
+  }
   // After quarter q has landed: bytes or nibbles -> words in place (every
   // lane's reads precede the wave's writes), and zero V rows for keys at or
   // past `valid` (their slots may hold anything, and 0 * NaN would poison

@@ -254,6 +254,8 @@ ekv_status ekv_attn_decode_shared(const ekv_pool* pool, const ekv_batch* prefixe
     a.log2_group = __builtin_ctz((unsigned)group);
     a.out_fp32 = out_dtype == EKV_DTYPE_FP32;
     a.grid = std::max(4, std::min(l.grid, resident));
+    if (batch->batch > 64 * a.grid)   // (each workgroup describes 64 sequences to the merge)
+      return fail(EKV_ERR_UNSUPPORTED, "ekv_attn_decode_shared: at most %d sequences", 64 * a.grid);
     a.min_units = l.min_units;
     a.scale_log2 = log2e_scale(scale);
     const bool elastic = (prefixes->batch > 0 && prefixes->mode != EKV_MODE_NATIVE) || batch->mode != EKV_MODE_NATIVE;

@@ -9,20 +9,20 @@
 // sequence's own, are joined by the merge kernel:
 //   out = sum_k 2^(m_k - M) o_k / sum_k 2^(m_k - M) l_k,  M = max_k m_k.
 //
-// One launch works on four kinds of segments (a segment: one KV head of a prefix, or of
+// One launch works on three kinds of segments (a segment: one KV head of a prefix, or of
 // a sequence's own tokens), each kind on workgroups of its own:
-//   team   a prefix with more than 128 query columns (sequence of the group, head of the
+//   team   a prefix with more than 32 query columns (sequence of the group, head of the
 //          KV head's G): a team of workgroups, one for each tile of 128 columns, takes a
-//          run of the prefix's units, so that all of the team read the same K and V at
-//          the same time, on one XCD;
-//   single a prefix with 33 to 128 columns: one workgroup takes a run of units;
+//          run of a segment's units, so that all of the team read the same K and V at
+//          the same time, on one XCD.  In a tile 4 waves x 32 columns share every unit,
+//          pipelined as in prefill.hip;
 //   few    a prefix with at most 32 columns: a wave streams its units alone;
 //   own    a sequence's own tokens, G columns: likewise.
-// In a tile of 128, 4 waves x 32 columns share every unit, pipelined as in prefill.hip.
-// The workgroups are divided between the kinds by the work that each has.  A kind's
-// units are one flat space (for teams, each prefix's are), a worker takes an equal run
-// of it and crosses segments.  Piece k of a segment is therefore made by worker
-// w_first + k, and its slot of partials follows from the segment and the worker.
+// The workgroups are divided between the kinds by the work that each has.  Units of few
+// and own are one flat space each, a wave takes an equal run of it and crosses segments;
+// a team stays in one segment where that costs little (a start costs as much as 5
+// units), else it crosses the KV heads of its prefix.  Piece k of a segment is therefore
+// made by worker w_first + k, and its slot of partials follows from segment and worker.
 #include <algorithm>
 #include <atomic>
 
@@ -38,70 +38,110 @@ constexpr int kTileCols = kWaves * kPfCols;
 // LDS: 4 slots of K planes and 5 of V planes of a unit (tiles), or a unit's slot per wave (few, own).
 constexpr int kVSlots = 5;
 constexpr int kVRing = 4 * kPlanePf;
-constexpr int kLdsBytes = kVRing + kVSlots * kPlanePf;
-static_assert(kLdsBytes >= kWaves * kSlotPf, "a slot for every wave");
+constexpr int kLdsRing = kVRing + kVSlots * kPlanePf;
+constexpr int kLdsBytes = kLdsRing + kWaves * 64 * 16;   // and 16 bytes a lane (the first rows read)
+static_assert(kLdsRing >= kWaves * kSlotPf, "a slot for every wave");
+static_assert(2 * kLdsBytes <= 160 * 1024, "two workgroups a CU");
 
 __device__ __forceinline__ int clamp_to(int x, int lo, int hi) { return min(max(x, lo), hi); }
 // The reference of a column all of whose scores so far are -inf: its weights are then 0, not NaN.
 __device__ __forceinline__ float finite_or_zero(float m) { return m == -__builtin_inff() ? 0.f : m; }
 __device__ __forceinline__ int units_of(int len) { return (len + 2 * kPage - 1) / (2 * kPage); }
 
-enum Kind { kNone, kFew, kSingle, kTeam };
+// The lane, opaque: what follows from it is computed where it is used, not kept in
+// registers from before a loop.
+__device__ __forceinline__ int fresh(int lane) {
+  asm volatile("" : "+v"(lane));
+  return lane;
+}
+__device__ __forceinline__ int lane_value(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
 
-// What the prefixes before a chunk of 64 amount to.
-struct GroupSums {
-  int chunk = 0;                           // the chunk's first prefix
-  int start = 0;                           // the group boundary so far
-  int few_units = 0, few_segments = 0;     // (a few segment has one slot, besides one a worker)
-  int single_units = 0, single_segments = 0, single_slots = 0;
-  int team_units = 0, team_tiles = 0, team_slots = 0, team_workers = 0;
+enum Kind { kNone, kFew, kTeam };
+
+// Sum over the lanes, and each lane's sum of the lanes before it.  Most launches have
+// one prefix (one lane that is not 0), which needs no scan.
+struct LaneSum {
+  int total, before;
+  __device__ __forceinline__ explicit LaneSum(int x) : total(0), before(0) {
+    const uint64_t some = __builtin_amdgcn_ballot_w64(x != 0);
+    if (some & (some - 1)) {
+      const int incl = sum_scan(x);
+      before = incl - x;
+      total = last_lane(incl);
+    } else if (some) {
+      total = lane_value(x, __builtin_ctzll(some));
+    }
+  }
 };
 
-// 64 prefixes, one a lane: their sequences, units, kind, and where their work and
-// slots begin in their kind's.  The group boundaries are clamped into the batch and
-// made nondecreasing, so that groups never overlap.
+// 64 prefixes, one a lane, as read: boundaries and length.
+struct GroupRow {
+  int start, end, len;
+  __device__ __forceinline__ GroupRow(int s, int e, int l) : start(s), end(e), len(l) {}
+  __device__ __forceinline__ GroupRow(const SharedArgs& a, int chunk, int lane) {
+    const int p = chunk + lane;
+    const bool in = p < a.prefix.rows;
+    start = in ? clamp_to(a.starts[p], 0, a.own.rows) : a.own.rows;
+    end = in ? clamp_to(a.starts[p + 1], 0, a.own.rows) : a.own.rows;
+    len = in ? clamp_to(a.prefix.lens[p], 0, a.prefix.len_cap) : 0;
+  }
+};
+
+// Their sequences, units and kind.  The group boundaries are clamped into the batch
+// and made nondecreasing (`from`: the boundary so far, advanced), so that groups
+// never overlap.
 struct Groups {
   int start, count, units, len, kind;
   int tiles, wide;                         // tiles of 128 and groups of 32 columns
-  int base, slot;                          // few, single: first unit; team: first worker; first slot
-  int run;                                 // team: units of the prefix (all KV heads) that a team takes
 
-  // the chunk at `sums`, with teams of about team_run units; advances `sums` past it
-  __device__ __forceinline__ Groups(const SharedArgs& a, GroupSums& sums, int team_run, int lane) {
-    const int p = sums.chunk + lane, hkv = a.num_kv_heads;
-    const bool in = p < a.prefix.rows;
-    const int s0 = in ? clamp_to(a.starts[p], 0, a.own.rows) : 0, s1 = in ? clamp_to(a.starts[p + 1], 0, a.own.rows) : 0;
-    len = in ? clamp_to(a.prefix.lens[p], 0, a.prefix.len_cap) : 0;
-    start = max(max_scan(s0), sums.start);
-    const int end = max(start, s1);
-    count = in ? end - start : 0;
+  __device__ __forceinline__ Groups(const SharedArgs& a, const GroupRow& r, int& from) {
+    start = r.start;
+    int end = r.end;
+    if (__builtin_amdgcn_ballot_w64(end < start || start < from)) {   // (boundaries that fall)
+      start = max(max_scan(start), from);
+      end = max(start, end);
+      from = last_lane(max_scan(end));
+    } else {
+      from = last_lane(end);
+    }
+    len = r.len;
+    count = len > 0 ? end - start : 0;
     const int columns = count << a.log2_group;
-    units = columns > 0 ? units_of(len) : 0;
+    units = count > 0 ? units_of(len) : 0;
     tiles = (columns + kTileCols - 1) / kTileCols;
     wide = (columns + kPfCols - 1) / kPfCols;
-    kind = units == 0 ? kNone : (columns <= kPfCols ? kFew : (tiles == 1 ? kSingle : kTeam));
-    const int all = hkv * units;
-    const int teams = kind == kTeam ? (all + team_run - 1) / team_run : 1;
-    run = (all + teams - 1) / teams;
-    const int few = kind == kFew ? all : 0, single = kind == kSingle ? all : 0, workers = kind == kTeam ? teams * tiles : 0;
-    const int single_slot = kind == kSingle ? hkv * wide : 0, team_slot = kind == kTeam ? (hkv + teams) * wide : 0;
-    const int if_u = sum_scan(few), if_s = sum_scan(kind == kFew ? hkv : 0), is_u = sum_scan(single), is_s = sum_scan(single_slot);
-    const int it_w = sum_scan(workers), it_s = sum_scan(team_slot);
-    base = kind == kFew ? sums.few_units + if_u - few
-                        : (kind == kSingle ? sums.single_units + is_u - single : sums.team_workers + it_w - workers);
-    slot = kind == kFew ? sums.few_segments + if_s - hkv
-                        : (kind == kSingle ? sums.single_slots + is_s - single_slot : sums.team_slots + it_s - team_slot);
-    sums.chunk += 64;
-    sums.few_units += last_lane(if_u);
-    sums.few_segments += last_lane(if_s);
-    sums.single_units += last_lane(is_u);
-    sums.single_segments += hkv * __builtin_popcountll(__builtin_amdgcn_ballot_w64(kind == kSingle));
-    sums.single_slots += last_lane(is_s);
-    sums.team_units += last_lane(sum_scan(kind == kTeam ? all * tiles : 0));
-    sums.team_tiles += last_lane(sum_scan(kind == kTeam ? tiles : 0));
-    sums.team_workers += last_lane(it_w);
-    sums.team_slots += last_lane(it_s);
-    sums.start = last_lane(max(max_scan(end), sums.start));
+    kind = units == 0 ? kNone : (columns <= kPfCols ? kFew : kTeam);
+  }
+};
+
+// A prefix's teams: `spans` of `span` units, each cut into `cuts` runs of `run`.
+struct Teams {
+  int span, cuts, run;
+  __device__ __forceinline__ Teams(const SharedPlan& plan, int units, int hkv) {
+    span = plan.team_aligned ? units : hkv * units;
+    cuts = (span + plan.team_run - 1) / plan.team_run;
+    run = cuts > 0 ? (span + cuts - 1) / cuts : 1;
+  }
+};
+
+// Where the work and the slots of 64 prefixes of one kind begin: units (few) or workers
+// (team), and slots.  `work` and `slots` count those before, and are advanced.
+struct Places {
+  int base, end, slot;
+  __device__ __forceinline__ Places(const Groups& x, const SharedPlan& plan, int kind, int hkv, int& work, int& slots) {
+    int w = hkv * x.units, n = hkv;   // few: a slot for each segment (and one for each worker)
+    if (kind == kTeam) {
+      const Teams t(plan, x.units, hkv);
+      w = (plan.team_aligned ? hkv : 1) * t.cuts * x.tiles;
+      n = (plan.team_aligned ? hkv * t.cuts : hkv + t.cuts) * x.wide;
+    }
+    const bool mine = x.kind == kind;
+    const LaneSum sw(mine ? w : 0), sn(mine ? n : 0);
+    base = work + sw.before;
+    end = mine ? base + w : base;
+    slot = slots + sn.before;
+    work += sw.total;
+    slots += sn.total;
   }
 };
 
@@ -109,11 +149,13 @@ struct Groups {
 struct SequenceSums {
   int chunk = 0, units = 0;
 };
+__device__ __forceinline__ int own_length(const SharedArgs& a, int s) {
+  return s < a.own.rows ? clamp_to(a.own.lens[s], 0, a.own.len_cap) : 0;
+}
 struct Sequences {
   int len, units, base;
-  __device__ __forceinline__ Sequences(const SharedArgs& a, SequenceSums& sums, int lane) {
-    const int s = sums.chunk + lane;
-    len = s < a.own.rows ? clamp_to(a.own.lens[s], 0, a.own.len_cap) : 0;
+  // (length: of sequence chunk + lane)
+  __device__ __forceinline__ Sequences(const SharedArgs& a, SequenceSums& sums, int length) : len(length) {
     units = units_of(len);
     const int n = a.num_kv_heads * units, incl = sum_scan(n);
     base = sums.units + incl - n;
@@ -121,8 +163,6 @@ struct Sequences {
     sums.units += last_lane(incl);
   }
 };
-
-__device__ __forceinline__ int lane_value(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
 
 // A run of units of one segment, as a worker meets it.
 struct Piece {
@@ -185,11 +225,9 @@ struct Worker {
   const SharedArgs& a;
   char* ring;
   int wave, lane, h;
-  Stager<F8> stager;
 
-  __device__ __forceinline__ Worker(const SharedArgs& a_, char* ring_)
-      : a(a_), ring(ring_), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), lane(threadIdx.x & 63),
-        h((threadIdx.x & 63) >> 5), stager(threadIdx.x & 63, a_.num_kv_heads) {}
+  __device__ __forceinline__ Worker(const SharedArgs& a_, char* ring_, int wave_, int lane_)
+      : a(a_), ring(ring_), wave(wave_), lane(lane_), h(lane_ >> 5) {}
 
   // the 32 columns from `first` on of a piece: sequence seq0 + column / G, head column % G of the KV head
   __device__ __forceinline__ void place(ColumnState<T>& col, const Piece& x, int first) const {
@@ -225,6 +263,7 @@ struct Worker {
   // units come from HBM, not from an L2 that sixteen query tiles have warmed.)
   __device__ __forceinline__ void tile(const Piece& x) {
     ColumnState<T> col;
+    const Stager<F8> stager(lane, a.num_kv_heads);
     place(col, x, wave * kPfCols);
     col.load_queries(a.q, a.scale_log2, h);
     const bool active = wave * kPfCols < x.columns;
@@ -318,20 +357,21 @@ struct Worker {
 
   // One wave's columns over a run of units, alone, in the wave's own slot of LDS.
   // `next` gives the run's pieces one after the other, at most 64 units each, and
-  // is asked one piece ahead: the block table of a piece is read while the one before
-  // is worked on, its first unit is loaded and its queries read when the last unit
-  // before has left the slot and the query registers, so that the wave's stream of
-  // loads does not stop between segments.
+  // is asked two ahead: while piece x is worked on, the block table of y is in
+  // registers, or y's first unit in flight and the table of z on its way.  A piece's
+  // first unit is loaded and its queries read as soon as the last unit before it
+  // has left the slot and the query registers, so that the wave's stream of loads does
+  // not stop between segments.
   template <typename Next>
   __device__ __forceinline__ void stream(const SharedPart& part, Next next, float* o, float* ml, int slots, int width) {
     ColumnState<T> col;
+    const Stager<F8> stager(lane, a.num_kv_heads);
     char* slot = ring + wave * kSlotPf;
     const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)(lds_ptr)slot);
     const uint32_t k_at = k_read_offset(lane), v_at = v_read_offset(lane);
     UnitTable<ELASTIC, F8> table(part);
-    Piece x, y;               // the piece of the unit at hand, and the one after it
-    bool more = next(x);
-    if (!more) return;
+    Piece x, y;
+    if (!next(x)) return;
     table.fetch(part, x, lane);
     table.enter(lane, x);
     bool base = false;
@@ -343,7 +383,7 @@ struct Worker {
     place(col, x, 0);
     issue(0);
     col.load_queries(a.q, a.scale_log2, h);
-    more = next(y);
+    bool more = next(y);      // y: the piece after x
     if (more) table.fetch(part, y, lane);
     int i = 0;                // unit of the piece
 #pragma unroll 1
@@ -359,11 +399,15 @@ struct Worker {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the slot has been read
       const bool last = x.u0 + ++i == x.u1;   // the piece's last unit
       const float c = col.mask(sc, key0, h);
+      Piece z;
+      bool beyond = false;
       if (!last) {
         issue(i);
       } else if (more) {
         table.enter(lane, y);
         issue(0);
+        beyond = next(z);
+        if (beyond) table.fetch(part, z, lane);
       }
       float shift;
       if (col.advance(sc, c, &shift)) col.rescale(shift == shift ? fast_exp2(shift) : 1.0f);
@@ -384,9 +428,9 @@ struct Worker {
         col.l = 0.f;
       }
       x = y;
+      y = z;
+      more = beyond;
       i = 0;
-      more = next(y);
-      if (more) table.fetch(part, y, lane);
     }
   }
 };
@@ -403,43 +447,44 @@ struct Describe {
   int4 own;     // off, units, run (0: none), 0
 };
 
-__device__ __forceinline__ void describe(const SharedArgs& a, const SharedPlan& plan, int team_slot0, int few_slot0, int chunk,
-                                         int lane) {
-  const int s = 64 * chunk + lane, hkv = a.num_kv_heads;
-  Describe d{int4{0, 0, 0, 0}, int4{0, 0, 1, 0}, int4{0, 0, 0, 0}};
-  GroupSums gs;
+// The prefix's part, for the sequences of chunk `chunk` (one a lane) that stand behind
+// the 64 prefixes x of one kind; slot0: that kind's first slot.
+__device__ __forceinline__ void describe_prefix(Describe& d, const SharedArgs& a, const SharedPlan& plan, const Groups& x,
+                                                const Places& at, int kind, int slot0, int chunk, int lane) {
+  const int s = 64 * chunk + lane;
+  uint64_t some = __builtin_amdgcn_ballot_w64(x.kind == kind && x.start < 64 * (chunk + 1) && x.start + x.count > 64 * chunk);
 #pragma unroll 1
-  while (gs.chunk < a.prefix.rows) {
-    const Groups x(a, gs, plan.team_run, lane);
-    uint64_t some = __builtin_amdgcn_ballot_w64(x.kind != kNone && x.start < 64 * (chunk + 1) && x.start + x.count > 64 * chunk);
-    while (some) {   // the prefixes whose groups reach into these sequences
-      const int l = __builtin_ctzll(some);
-      some &= some - 1;
-      const int start = lane_value(x.start, l), units = lane_value(x.units, l), kind = lane_value(x.kind, l);
-      const int base = lane_value(x.base, l), slot = lane_value(x.slot, l), wide = lane_value(x.wide, l);
-      const int j = (s - start) << a.log2_group;
-      if (s >= start && s < start + lane_value(x.count, l)) {
-        d.units = int4{kind == kTeam ? 0 : base, units, units,
-                       kind == kTeam ? lane_value(x.run, l) : (kind == kSingle ? plan.single_run : plan.few_run)};
-        if (kind == kFew) d.slots = int4{few_slot0 + slot, 1, 1, j};
-        else d.slots = int4{(kind == kTeam ? team_slot0 : 0) + slot + j / kPfCols, wide, kind == kTeam ? wide : kWaves, j & (kPfCols - 1)};
-      }
+  while (some) {   // the prefixes whose groups reach into these sequences
+    const int l = __builtin_ctzll(some);
+    some &= some - 1;
+    const int start = lane_value(x.start, l), units = lane_value(x.units, l), wide = lane_value(x.wide, l);
+    const int base = lane_value(at.base, l), slot = slot0 + lane_value(at.slot, l);
+    if (s < start || s >= start + lane_value(x.count, l)) continue;
+    const int j = (s - start) << a.log2_group;
+    if (kind == kFew) {
+      d.units = int4{base, units, units, plan.few_run};
+      d.slots = int4{slot, 1, 1, j};
+    } else {
+      const Teams t(plan, units, a.num_kv_heads);
+      d.units = int4{0, plan.team_aligned ? t.cuts * t.run : units, units, t.run};
+      d.slots = int4{slot + j / kPfCols, plan.team_aligned ? 0 : wide, wide, j & (kPfCols - 1)};
     }
   }
-  // the units of the sequences before this chunk
-  int before = 0;
+}
+// The sequences' own part.
+__device__ __forceinline__ void describe_own(Describe& d, const SharedArgs& a, const SharedPlan& plan, int chunk, int lane) {
+  int before = 0;   // the units of the sequences before this chunk
 #pragma unroll 1
   for (int c = 0; c < 64 * chunk; c += 512) {
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
       const int t = c + 64 * u + lane;
-      before += units_of(t < 64 * chunk ? clamp_to(a.own.lens[t], 0, a.own.len_cap) : 0);
+      before += units_of(t < 64 * chunk ? own_length(a, t) : 0);
     }
   }
-  SequenceSums ss{64 * chunk, hkv * last_lane(sum_scan(before))};
-  const Sequences y(a, ss, lane);
+  SequenceSums ss{64 * chunk, a.num_kv_heads * last_lane(sum_scan(before))};
+  const Sequences y(a, ss, own_length(a, 64 * chunk + lane));
   if (y.units > 0) d.own = int4{y.base, y.units, plan.own_run, 0};
-  if (s < a.own.rows) reinterpret_cast<Describe*>(a.plan)[s] = d;
 }
 
 // ---- the kernel ---------------------------------------------------------------
@@ -447,166 +492,213 @@ __device__ __forceinline__ void describe(const SharedArgs& a, const SharedPlan& 
 template <typename T, bool ELASTIC, bool F8>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void shared_kernel(SharedArgs a) {
   __shared__ __attribute__((aligned(16))) char ring[kLdsBytes];
-  Worker<T, ELASTIC, F8> worker(a, ring);
-  const int lane = worker.lane, hkv = a.num_kv_heads;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hkv = a.num_kv_heads;
 
-  // the work of each kind
-  GroupSums g;
+  // (the first 64 prefixes and sequences are read once and kept in LDS, a copy for every wave)
+  int4* rows0 = reinterpret_cast<int4*>(ring + kLdsRing) + 64 * wave + lane;
+  int own_units, own_rows;   // (rows with tokens)
+  {
+    const GroupRow r(a, 0, lane);
+    const int len0 = own_length(a, lane);
+    *rows0 = int4{r.start, r.end, r.len, len0};
+    own_units = units_of(len0);
+    own_rows = len0 > 0 ? 1 : 0;
+  }
 #pragma unroll 1
-  while (g.chunk < a.prefix.rows) Groups(a, g, 1, lane);
-  int own_units = 0, own_rows = 0;   // (rows with tokens)
-#pragma unroll 1
-  for (int c = 0; c < a.own.rows; c += 512) {   // (8 loads in flight)
+  for (int c = 64; c < a.own.rows; c += 512) {   // (8 loads in flight)
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-      const int s = c + 64 * u + lane;
-      const int n = units_of(s < a.own.rows ? clamp_to(a.own.lens[s], 0, a.own.len_cap) : 0);
+      const int n = units_of(own_length(a, c + 64 * u + lane));
       own_units += n;
       own_rows += n > 0 ? 1 : 0;
     }
   }
   own_units = hkv * last_lane(sum_scan(own_units));
   own_rows = last_lane(sum_scan(own_rows));
-  const SharedPlan plan = divide_work(
-      SharedWork{g.team_units, g.team_tiles, hkv * g.team_tiles, g.single_units, g.single_segments, g.few_units, g.few_segments, own_units, hkv * own_rows},
-      (int)gridDim.x, a.min_units, F8);
-  // slots: of the singles, of the teams, of the few
-  const int team_slot0 = g.single_slots + kWaves * plan.single_workers;
-  GroupSums t;
-  if (plan.team_workers > 0) {
-#pragma unroll 1
-    while (t.chunk < a.prefix.rows) Groups(a, t, plan.team_run, lane);
-  }
-  const int few_slot0 = team_slot0 + t.team_slots;
 
-  // What the merge needs, per sequence, written by the last workgroups, 64 sequences each.
-  for (int c = gridDim.x - 1 - blockIdx.x; 64 * c < a.own.rows && worker.wave == 0; c += gridDim.x)
-    describe(a, plan, team_slot0, few_slot0, c, lane);
-
-  // a prefix, found by its kind and a unit (team: a worker); the search goes on where it ended
-  struct {
-    int p = -1, start, count, units, len, tiles, wide, base, slot, run, end;
-  } at;
-  GroupSums gs;
-  auto find_prefix = [&](int pos, int kind) -> bool {
-    if (at.p >= 0 && pos < at.end) return true;
+  // One loop scans the prefixes and works, so that the code of either is there once (a
+  // launch starts with a cold instruction cache): pass 0 adds up the work of each kind
+  // and divides the workers; pass 1 describes sequences to the merge and finds this
+  // worker's first prefix; later ones find the next prefix.
+  SharedPlan plan{};
+  int kind = kNone;              // of this worker (kNone: a wave for the sequences' own tokens)
+  int id = 0, pos = 0, end = 0;  // its number in its kind (few, own: this wave's); its units (team: its number)
+  int few_units = 0, team_units = 0, team_tiles = 0, few_segments = 0, team_slot0 = 0;   // (the few's slots come first)
 #pragma unroll 1
-    while (gs.chunk < a.prefix.rows) {
-      const GroupSums before = gs;
-      const Groups x(a, gs, plan.team_run, lane);
-      const int all = hkv * x.units, end = x.base + (kind == kTeam ? (all + x.run - 1) / max(x.run, 1) * x.tiles : all);
-      const uint64_t hit = __builtin_amdgcn_ballot_w64(x.kind == kind && x.base <= pos && pos < end);
-      if (!hit) continue;
+  for (int pass = 0;; ++pass) {
+    struct {
+      int p, start, count, units, len, tiles, wide, base, slot, end;
+    } at{};
+    bool found = pass > 0 && kind == kNone;
+    const int chunk = gridDim.x - 1 - blockIdx.x;   // the last workgroups describe 64 sequences each
+    const bool describes = pass == 1 && wave == 0 && 64 * chunk < a.own.rows;
+    Describe d{int4{0, 0, 0, 0}, int4{0, 0, 1, 0}, int4{0, 0, 0, 0}};
+    int from = 0, work = 0, slots = 0, other_work = 0, other_slots = 0;
+#pragma unroll 1
+    for (int c0 = 0; c0 < a.prefix.rows && (pass < 2 || !found); c0 += 64) {
+      GroupRow r(0, 0, 0);
+      if (c0 == 0) {
+        const int4 v = *rows0;
+        r = GroupRow(v.x, v.y, v.z);
+      } else {
+        r = GroupRow(a, c0, lane);
+      }
+      const Groups x(a, r, from);
+      if (pass == 0) {
+        const bool team = x.kind == kTeam;
+        few_units += LaneSum(x.kind == kFew ? hkv * x.units : 0).total;
+        few_segments += hkv * __builtin_popcountll(__builtin_amdgcn_ballot_w64(x.kind == kFew));
+        team_units += LaneSum(team ? hkv * x.tiles * x.units : 0).total;
+        team_tiles += LaneSum(team ? x.tiles : 0).total;
+        continue;
+      }
+      if (describes) {
+        const int other = kind == kTeam ? kFew : kTeam;   // (own workers: both kinds, one here and one below)
+        const Places y(x, plan, other, hkv, other_work, other_slots);
+        describe_prefix(d, a, plan, x, y, other, other == kTeam ? team_slot0 : 0, chunk, lane);
+      }
+      const int mine = kind == kNone ? kFew : kind;
+      const Places y(x, plan, mine, hkv, work, slots);
+      if (describes) describe_prefix(d, a, plan, x, y, mine, mine == kTeam ? team_slot0 : 0, chunk, lane);
+      const uint64_t hit = __builtin_amdgcn_ballot_w64(x.kind == mine && y.base <= pos && pos < y.end);
+      if (found || !hit) continue;
+      found = true;
       const int l = __builtin_ctzll(hit);
-      at.p = before.chunk + l;
+      at.p = c0 + l;
       at.start = lane_value(x.start, l);
       at.count = lane_value(x.count, l);
       at.units = lane_value(x.units, l);
       at.len = lane_value(x.len, l);
       at.tiles = lane_value(x.tiles, l);
       at.wide = lane_value(x.wide, l);
-      at.base = lane_value(x.base, l);
-      at.slot = lane_value(x.slot, l);
-      at.run = lane_value(x.run, l);
-      at.end = lane_value(end, l);
-      gs = before;   // (the next prefix may lie in this chunk)
-      return true;
+      at.base = lane_value(y.base, l);
+      at.slot = lane_value(y.slot, l);
+      at.end = lane_value(y.end, l);
     }
-    return false;   // (lengths that changed under the launch)
-  };
-
-  const int w = blockIdx.x;
-  if (w < plan.team_workers + plan.single_workers) {
-    const bool team = w < plan.team_workers;
-    // team workers in order of (prefix, team, tile), neighbours on one XCD (ids go round robin over the 8)
-    const int q = plan.team_workers / 8, r = plan.team_workers % 8, xcd = w % 8;
-    int id = team ? xcd * q + min(xcd, r) + w / 8 : w - plan.team_workers;
-#pragma unroll 1
-    for (bool again = true; again; ) {
-      int tile = 0, slot0 = 0, pos, end;   // units: of the prefix (team), or of all singles
-      if (team) {
-        if (id >= t.team_workers || !find_prefix(id, kTeam)) break;
-        const int m = (id - at.base) / at.tiles;
-        tile = (id - at.base) - m * at.tiles;
-        pos = m * at.run;
-        end = min(hkv * at.units, pos + at.run);
-        slot0 = team_slot0 + at.slot + m * at.wide;
-        id += plan.team_workers;
+    if (pass == 0) {
+      plan = divide_work(SharedWork{team_units, team_tiles, hkv * team_tiles, few_units, few_segments, own_units, hkv * own_rows},
+                         (int)gridDim.x, a.min_units, F8);
+      team_slot0 = few_segments + kWaves * plan.few_workers;
+      id = blockIdx.x;
+      if (id < plan.team_workers) {
+        // team workers in order of (prefix, segment, run, tile), neighbours on one XCD (ids go round robin over the 8)
+        const int q = plan.team_workers / 8, r = plan.team_workers % 8;
+        kind = kTeam;
+        id = id % 8 * q + min(id % 8, r) + id / 8;
+        pos = id;
+        end = pos + 1;
       } else {
-        pos = id * plan.single_run;
-        end = min(g.single_units, pos + plan.single_run);
-        again = false;
+        id -= plan.team_workers;
+        kind = id < plan.few_workers ? kFew : kNone;
+        if (kind == kNone) id -= plan.few_workers;
+        id = id * kWaves + wave;
+        const int run = kind == kFew ? plan.few_run : plan.own_run;
+        pos = id * run;
+        end = min(kind == kFew ? few_units : own_units, pos + run);
       }
+      continue;
+    }
+    if (describes) {
+      describe_own(d, a, plan, chunk, lane);
+      if (64 * chunk + lane < a.own.rows) reinterpret_cast<Describe*>(a.plan)[64 * chunk + lane] = d;
+    }
+    if (!found || pos >= end) return;
+
+    if (kind == kTeam) {
+      const Teams t(plan, at.units, hkv);
+      const int team = (pos - at.base) / at.tiles, tile = (pos - at.base) - team * at.tiles;
+      const int k = team / t.cuts, first = tile * kTileCols;   // span; first column
+      int u = k * t.span + (team - k * t.cuts) * t.run;
+      const int u_end = min((k + 1) * t.span, u + t.run);
 #pragma unroll 1
-      while (pos < end && (team || find_prefix(pos, kSingle))) {
-        const int off = team ? pos : pos - at.base;
-        const int first = tile * kTileCols;
+      while (u < u_end) {
         Piece pc;
         pc.row = at.p;
-        pc.kvh = off / at.units;
+        pc.kvh = u / at.units;
         pc.len = at.len;
-        pc.u0 = off - pc.kvh * at.units;
-        pc.u1 = min(at.units, pc.u0 + (end - pos));
+        pc.u0 = u - pc.kvh * at.units;
+        pc.u1 = min(at.units, pc.u0 + (u_end - u));
         pc.seq0 = at.start + (first >> a.log2_group);
         pc.columns = min((at.count << a.log2_group) - first, kTileCols);
-        pc.slot = pc.kvh * at.wide + kWaves * tile + (team ? slot0 : at.slot + kWaves * id);
-        worker.tile(pc);
-        pos += pc.u1 - pc.u0;
+        pc.slot = team_slot0 + at.slot + (team + (plan.team_aligned ? 0 : pc.kvh)) * at.wide + kWaves * tile;
+        Worker<T, ELASTIC, F8>(a, ring, wave, fresh(lane)).tile(pc);
+        u += pc.u1 - pc.u0;
       }
+      pos += plan.team_workers;   // (more of the prefixes' tiles than workers: another round)
+      end = pos + 1;
+      continue;
     }
-    return;
-  }
 
-  // a wave's units: of the prefixes with few columns, or of the sequences
-  const bool few = w < plan.team_workers + plan.single_workers + plan.few_workers;
-  const int ww = (w - plan.team_workers - plan.single_workers - (few ? 0 : plan.few_workers)) * kWaves + worker.wave;
-  int pos = ww * (few ? plan.few_run : plan.own_run);
-  const int end = min(few ? g.few_units : own_units, pos + (few ? plan.few_run : plan.own_run));
-  SequenceSums ss;
-  auto find_sequence = [&](int u) -> bool {
-    if (at.p >= 0 && u < at.end) return true;
+    // a wave's units of one prefix, or of the sequences
+    const bool few = kind == kFew;
+    int u = pos;
+    const int u_end = few ? min(end, at.end) : end;
+    int seqs = 0, lane_at = 0, lens = rows0->w;   // own: the chunk of sequences at hand, the one in it, the lengths
+    if (!few) {
+      SequenceSums ss;
+      uint64_t hit = 0;
 #pragma unroll 1
-    while (ss.chunk < a.own.rows) {
-      const SequenceSums before = ss;
-      const Sequences y(a, ss, lane);
-      const uint64_t hit = __builtin_amdgcn_ballot_w64(y.base <= u && u < y.base + hkv * y.units);
-      if (!hit) continue;
-      const int l = __builtin_ctzll(hit);
-      at.p = before.chunk + l;
-      at.len = lane_value(y.len, l);
-      at.units = lane_value(y.units, l);
-      at.base = lane_value(y.base, l);
-      at.end = at.base + hkv * at.units;
-      ss = before;
-      return true;
+      while (!hit && ss.chunk < a.own.rows) {
+        seqs = ss.chunk;
+        if (seqs > 0) lens = own_length(a, seqs + lane);
+        const Sequences y(a, ss, lens);
+        hit = __builtin_amdgcn_ballot_w64(y.base <= u && u < y.base + hkv * y.units);
+        if (!hit) continue;
+        lane_at = __builtin_ctzll(hit);
+        at.base = lane_value(y.base, lane_at);
+        at.end = at.base;   // (set below)
+      }
+      if (!hit) return;     // (lengths that changed under the launch)
     }
-    return false;
-  };
-  const SharedPart part = few ? a.prefix : a.own;
-  auto next = [&](Piece& x) -> bool {
-    if (pos >= end || !(few ? find_prefix(pos, kFew) : find_sequence(pos))) return false;
-    const int off = pos - at.base;
-    x.row = at.p;
-    x.len = at.len;
-    x.kvh = off / at.units;
-    x.u0 = off - x.kvh * at.units;
-    x.u1 = min(at.units, x.u0 + min(64, end - pos));
-    x.seq0 = few ? at.start : at.p;
-    x.columns = (few ? at.count : 1) << a.log2_group;
-    x.slot = (few ? few_slot0 + at.slot : at.p * hkv) + x.kvh + ww;
-    pos += x.u1 - x.u0;
-    return true;
-  };
-  worker.stream(part, next, few ? a.o_wide : a.o_own, few ? a.ml_wide : a.ml_own, few ? a.wide_slots : a.own_slots,
-                few ? kPfCols : 1 << a.log2_group);
+    bool enter = !few;
+    auto next = [&](Piece& x) -> bool {
+      if (u >= u_end) return false;
+      if (!few && (enter || u >= at.end)) {
+        if (!enter) {       // the next sequence that has tokens
+          at.base = at.end;
+          uint64_t left = lane_at == 63 ? 0 : __builtin_amdgcn_ballot_w64(lens > 0) & (~0ull << (lane_at + 1));
+#pragma unroll 1
+          while (!left) {
+            seqs += 64;
+            if (seqs >= a.own.rows) return false;
+            lens = own_length(a, seqs + lane);
+            left = __builtin_amdgcn_ballot_w64(lens > 0);
+          }
+          lane_at = __builtin_ctzll(left);
+        }
+        enter = false;
+        at.p = at.start = seqs + lane_at;
+        at.len = lane_value(lens, lane_at);
+        at.units = units_of(at.len);
+        at.end = at.base + hkv * at.units;
+        at.count = 1;
+        at.slot = at.p * hkv;
+      }
+      const int off = u - at.base;
+      x.row = at.p;
+      x.len = at.len;
+      x.kvh = off / at.units;
+      x.u0 = off - x.kvh * at.units;
+      x.u1 = min(at.units, x.u0 + min(64, u_end - u));
+      x.seq0 = at.start;
+      x.columns = at.count << a.log2_group;
+      x.slot = at.slot + x.kvh + id;
+      u += x.u1 - x.u0;
+      return true;
+    };
+    Worker<T, ELASTIC, F8>(a, ring, wave, fresh(lane)).stream(few ? a.prefix : a.own, next, few ? a.o_wide : a.o_own, few ? a.ml_wide : a.ml_own,
+                  few ? a.wide_slots : a.own_slots, few ? kPfCols : 1 << a.log2_group);
+    if (!few) return;
+    pos = u_end;
+  }
 }
 
 // ---- merge ---------------------------------------------------------------------
 // A workgroup joins 32 columns (32 / G sequences of one KV head): lane l holds
 // column l % 32, and wave w the chunks 4 w .. 4 w + 3 (2 each for l / 32).  Two
-// memory round trips for up to 8 pieces of each part: the sequence's description,
-// then maxima, sums and outputs together.
-constexpr int kMergeWaves = 8, kAtOnce = 8;
+// memory round trips for up to 8 pieces of the prefix and 4 of the sequence's own: the
+// sequence's description, then maxima, sums and outputs together.
+constexpr int kMergeWaves = 8;
 
 // running (max, sum, outputs) of a column's chunks
 struct Joined {
@@ -614,17 +706,18 @@ struct Joined {
   f32x4 o[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
 };
 
-// Joins `n` pieces (per lane), `slot`, `slot + step`, ..., of slots with `width` columns, column `col`.
-__device__ __forceinline__ void join(Joined& j, const float* os, const float* mls, int n, int slot, int step, int width, int col,
-                                     int slots, int chunk) {
-  const f32x4* op = reinterpret_cast<const f32x4*>(os);
-  const float2* mp = reinterpret_cast<const float2*>(mls);
-#pragma unroll 1
-  for (int k0 = 0; __builtin_amdgcn_ballot_w64(k0 < n); k0 += kAtOnce) {
-    float2 ml[kAtOnce];
-    f32x4 x[kAtOnce][2];
+// N pieces of a column, loaded together: those from k0 on of `n` (per lane) at `slot`,
+// `slot + step`, ..., of slots with `width` columns, column `col`.
+template <int N>
+struct Pieces {
+  float2 ml[N];
+  f32x4 x[N][2];
+  __device__ __forceinline__ Pieces(const float* os, const float* mls, int k0, int n, int slot, int step, int width, int col,
+                                    int slots, int chunk) {
+    const f32x4* op = reinterpret_cast<const f32x4*>(os);
+    const float2* mp = reinterpret_cast<const float2*>(mls);
 #pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) {
+    for (int k = 0; k < N; ++k) {
       const int at = slot + (k0 + k) * step;
       ml[k] = make_float2(-__builtin_inff(), 0.f);
       x[k][0] = x[k][1] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -634,16 +727,18 @@ __device__ __forceinline__ void join(Joined& j, const float* os, const float* ml
         for (int i = 0; i < 2; ++i) x[k][i] = op[((size_t)at * 32 + chunk + 2 * i) * width + col];
       }
     }
+  }
+  __device__ __forceinline__ void join(Joined& j) const {
     float top = j.m;
 #pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) top = fmaxf(top, ml[k].x);
+    for (int k = 0; k < N; ++k) top = fmaxf(top, ml[k].x);
     const float base = finite_or_zero(top);   // (no piece yet: every weight is 0)
     const float f = fast_exp2(j.m - base);
     j.l *= f;
 #pragma unroll
     for (int i = 0; i < 2; ++i) j.o[i] *= f;
 #pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) {
+    for (int k = 0; k < N; ++k) {
       const float e = fast_exp2(ml[k].x - base);
       j.l += e * ml[k].y;
 #pragma unroll
@@ -651,7 +746,7 @@ __device__ __forceinline__ void join(Joined& j, const float* os, const float* ml
     }
     j.m = top;
   }
-}
+};
 
 template <typename T>
 __global__ __launch_bounds__(64 * kMergeWaves) void shared_merge_kernel(SharedArgs a) {
@@ -673,8 +768,14 @@ __global__ __launch_bounds__(64 * kMergeWaves) void shared_merge_kernel(SharedAr
     own_slot = s * a.num_kv_heads + kvh + w0;
   }
   Joined j;
-  join(j, a.o_wide, a.ml_wide, wide_n, wide_slot, d.slots.z, kPfCols, d.slots.w + head, a.wide_slots, chunk);
-  join(j, a.o_own, a.ml_own, own_n, own_slot, 1, 1 << a.log2_group, head, a.own_slots, chunk);
+  constexpr int kWide = 8, kOwn = 4;
+#pragma unroll 1
+  for (int w0 = 0, o0 = 0; __builtin_amdgcn_ballot_w64(w0 < wide_n || o0 < own_n); w0 += kWide, o0 += kOwn) {
+    const Pieces<kWide> w(a.o_wide, a.ml_wide, w0, wide_n, wide_slot, d.slots.z, kPfCols, d.slots.w + head, a.wide_slots, chunk);
+    const Pieces<kOwn> o(a.o_own, a.ml_own, o0, own_n, own_slot, 1, 1 << a.log2_group, head, a.own_slots, chunk);
+    w.join(j);
+    o.join(j);
+  }
   const float inv = wide_n + own_n > 0 ? 1.0f / j.l : 0.f;   // (a sequence without any token: zeros)
   const size_t row = ((size_t)s * a.num_q_heads + (kvh << a.log2_group) + head) * kHeadDim;
 #pragma unroll
@@ -710,7 +811,7 @@ hipError_t shared_resident(int* workgroups) {
     if ((e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev)) != hipSuccess) return e;
     cache[dev].store(cus, std::memory_order_relaxed);
   }
-  *workgroups = 2 * cus;   // (74,880 B of LDS and at most 256 registers: two a CU)
+  *workgroups = 2 * cus;   // (78,976 B of LDS and at most 256 registers: two a CU)
   return hipSuccess;
 }
 

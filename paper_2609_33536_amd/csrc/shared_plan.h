@@ -3,6 +3,7 @@
 #pragma once
 
 #include <hip/hip_runtime.h>
+#include <math.h>
 #include <stdint.h>
 
 namespace ekv {
@@ -37,14 +38,14 @@ constexpr int kMaxSharedGrid = 512;
 
 // Units and segments of each kind; a team's count once for each of its tiles.
 struct SharedWork {
-  int team_units, team_tiles, team_segments, single_units, single_segments, few_units, few_segments, own_units, own_segments;
+  int team_units, team_tiles, team_segments, few_units, few_segments, own_units, own_segments;
 };
 
-// Workgroups of each kind, and the units that one takes (single), one of its 4
-// waves (few, own), or a team of them takes of a prefix, at most (team).
+// Workgroups of each kind, and the units that one of their waves takes (few, own), or
+// a team of them at most (team): of one segment (aligned) or of a prefix's segments.
 struct SharedPlan {
-  int team_workers, single_workers, few_workers, own_workers;
-  int team_run, single_run, few_run, own_run;
+  int team_workers, few_workers, own_workers;
+  int team_run, team_aligned, few_run, own_run;
 };
 
 // Divides `grid` workgroups (at least 4) over the kinds by their units and
@@ -53,25 +54,36 @@ struct SharedPlan {
 // segment costs its start (table, queries, first loads) and its partials.
 __host__ __device__ inline SharedPlan divide_work(const SharedWork& n, int grid, int min_units, bool bytes8) {
   const float stream = bytes8 ? 2.f : 3.f;
-  const float cost[4] = {4.f * n.team_units + 16.f * n.team_segments, 4.f * n.single_units + 16.f * n.single_segments,
-                         stream * n.few_units + 2.f * n.few_segments, stream * n.own_units + 2.f * n.own_segments};
-  const float all = cost[0] + cost[1] + cost[2] + cost[3], share = all > 0.f ? grid / all : 0.f;
-  int w[4], sum = 0, most = 0;
-  for (int i = 0; i < 4; ++i) {
-    w[i] = (int)(share * cost[i]);
-    if (cost[i] > 0.f && w[i] == 0) w[i] = 1;
-    sum += w[i];
-    if (cost[i] > cost[most]) most = i;
+  const float team = 4.f * n.team_units + 20.f * n.team_segments;
+  const float few = stream * n.few_units + 3.f * n.few_segments, own = stream * n.own_units + 3.f * n.own_segments;
+  const float share = grid / fmaxf(1.f, team + few + own);
+  int t = (int)(share * team), f = (int)(share * few), o = (int)(share * own);
+  if (n.team_units > 0 && t == 0) t = 1;
+  if (n.few_units > 0 && f == 0) f = 1;
+  if (n.own_units > 0 && o == 0) o = 1;
+  // (what rounding left over or took too much)
+  const int rest = grid - t - f - o;
+  if (t >= f && t >= o) t += rest;
+  else if (f >= o) f += rest;
+  else o += rest;
+  SharedPlan p{t, f, o, 1, 0, 1, 1};
+  if (n.few_units > 0) p.few_run = (n.few_units + 4 * f - 1) / (4 * f);
+  if (p.few_run < min_units) p.few_run = min_units;
+  if (n.own_units > 0) p.own_run = (n.own_units + 4 * o - 1) / (4 * o);
+  if (n.team_units > 0) {
+    // every prefix (or segment) rounds its number of teams up, which adds at most its tiles
+    const int half = (t + 1) / 2, free = t - n.team_tiles > half ? t - n.team_tiles : half;
+    p.team_run = (n.team_units + free - 1) / free;
+    if (t > n.team_segments) {
+      const int run = (n.team_units + t - n.team_segments - 1) / (t - n.team_segments);
+      if (run <= p.team_run + 5) {   // (a start costs a worker what 5 units do)
+        p.team_run = run;
+        p.team_aligned = 1;
+      }
+    }
   }
-  if (all > 0.f) w[most] += grid - sum;   // (what rounding left over or took too much)
-  auto run = [](int units, int workers, int least) -> int {
-    const int r = workers > 0 ? (units + workers - 1) / workers : 1;
-    return r > least ? r : least;
-  };
-  // teams: every prefix rounds its number of teams up, which adds at most its tiles to the workers
-  const int spare = w[0] - n.team_tiles, teams = spare > w[0] / 2 ? spare : (w[0] + 1) / 2;
-  return SharedPlan{w[0], w[1], w[2], w[3], run(n.team_units, teams, min_units), run(n.single_units, w[1], min_units),
-                    run(n.few_units, 4 * w[2], min_units), run(n.own_units, 4 * w[3], 1)};
+  if (p.team_run < min_units) p.team_run = min_units;
+  return p;
 }
 
 // Workgroups resident on the current device.

@@ -25,7 +25,7 @@ bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0;
 // and KV head, and 4 per workgroup for the segments that workers cut; likewise one
 // per sequence and KV head.
 struct SharedLayout {
-  int grid, min_units;
+  int grid, min_units, merge_ways;
   int64_t wide_slots, own_slots;
   size_t ml_wide, o_wide, ml_own, o_own, total;
 };
@@ -35,12 +35,19 @@ ekv_status plan_shared(const ekv_pool* p, const ekv_batch* prefixes, const ekv_b
   const int64_t groups = std::min<int64_t>(prefixes->batch, rows);
   const int64_t units_p = (max_seq_blocks(prefixes) + 1) / 2, units_s = (max_seq_blocks(b) + 1) / 2;
   const int64_t tiles = columns / 128 + groups;
-  const int64_t work_t = hkv * tiles * units_p, work_s = hkv * rows * units_s;
+  const int64_t work_t = hkv * tiles * (units_p + 1), work_s = hkv * rows * (units_s + 1);   // (a segment's start counts too)
   if (work_t >= (1 << 30) || work_s >= (1 << 30) || columns * hkv >= (1 << 30) || prefixes->batch >= (1 << 24))
     return fail(EKV_ERR_UNSUPPORTED, "batch too large for one shared-prefix decode call");
   l->min_units = (int)std::max<int64_t>(1, std::min<int64_t>(4, units_p / 16));   // (of the prefixes: pieces to merge)
-  const int64_t wanted = (work_t + hkv * groups * units_p / 4 + work_s / 4) / l->min_units + 4;
+  const int64_t wanted = (work_t + hkv * groups * (units_p + 1) / 4 + work_s / 4) / l->min_units + 4;
   l->grid = (int)std::min<int64_t>(kMaxSharedGrid, wanted);
+  // The merge: a workgroup takes 8 pieces a memory round trip.  Where a column may have more (at
+  // most its units, or what is left of the workers for each segment), up to 8 waves divide them, as
+  // long as that leaves the launch at most twice the device's workgroups.
+  const int64_t pieces = std::min(units_p / l->min_units, 4 * l->grid / std::max<int64_t>(1, hkv * groups)) +
+                         std::min(units_s, 4 * l->grid / std::max<int64_t>(1, hkv * rows));
+  l->merge_ways = 1;
+  while (l->merge_ways < 8 && pieces > 8 * l->merge_ways && (columns / 32 + 1) * hkv * 2 * l->merge_ways <= 512) l->merge_ways *= 2;
   l->wide_slots = hkv * (columns / 32 + groups) + columns / 32 + 4 * groups + 4 * l->grid;
   l->own_slots = hkv * rows + 4 * l->grid;
   auto align = [](size_t x) { return (x + 255) & ~(size_t)255; };
@@ -257,6 +264,7 @@ ekv_status ekv_attn_decode_shared(const ekv_pool* pool, const ekv_batch* prefixe
     if (batch->batch > 64 * a.grid)   // (each workgroup describes 64 sequences to the merge)
       return fail(EKV_ERR_UNSUPPORTED, "ekv_attn_decode_shared: at most %d sequences", 64 * a.grid);
     a.min_units = l.min_units;
+    a.merge_ways = l.merge_ways;
     a.scale_log2 = log2e_scale(scale);
     const bool elastic = (prefixes->batch > 0 && prefixes->mode != EKV_MODE_NATIVE) || batch->mode != EKV_MODE_NATIVE;
     return hip_status(launch_shared(a, pool->dtype, elastic, stream), "ekv_attn_decode_shared launch");

@@ -18,8 +18,9 @@
 //          pipelined as in prefill.hip;
 //   few    a prefix with at most 32 columns: a wave streams its units alone;
 //   own    a sequence's own tokens, G columns: likewise.
-// The workgroups are divided between the kinds by the work that each has.  Units of few
-// and own are one flat space each, a wave takes an equal run of it and crosses segments;
+// The workgroups are divided between the kinds by the work that each has.  The units of
+// few and own are one flat space each, in which a segment's start counts as a unit; a
+// wave takes an equal run of it and crosses segments;
 // a team stays in one segment where that costs little (a start costs as much as 5
 // units), else it crosses the KV heads of its prefix.  Piece k of a segment is therefore
 // made by worker w_first + k, and its slot of partials follows from segment and worker.
@@ -87,30 +88,34 @@ struct GroupRow {
   }
 };
 
-// Their sequences, units and kind.  The group boundaries are clamped into the batch
-// and made nondecreasing (`from`: the boundary so far, advanced), so that groups
-// never overlap.
-struct Groups {
+// What follows from a prefix's sequences and length.
+struct Shape {
   int start, count, units, len, kind;
   int tiles, wide;                         // tiles of 128 and groups of 32 columns
-
-  __device__ __forceinline__ Groups(const SharedArgs& a, const GroupRow& r, int& from) {
-    start = r.start;
-    int end = r.end;
-    if (__builtin_amdgcn_ballot_w64(end < start || start < from)) {   // (boundaries that fall)
-      start = max(max_scan(start), from);
-      end = max(start, end);
-      from = last_lane(max_scan(end));
-    } else {
-      from = last_lane(end);
-    }
-    len = r.len;
+  __device__ __forceinline__ Shape() {}
+  __device__ __forceinline__ Shape(int start_, int end, int len_, int log2_group) : start(start_), len(len_) {
     count = len > 0 ? end - start : 0;
-    const int columns = count << a.log2_group;
+    const int columns = count << log2_group;
     units = count > 0 ? units_of(len) : 0;
     tiles = (columns + kTileCols - 1) / kTileCols;
     wide = (columns + kPfCols - 1) / kPfCols;
     kind = units == 0 ? kNone : (columns <= kPfCols ? kFew : kTeam);
+  }
+};
+
+// Of 64 prefixes.  The group boundaries are clamped into the batch and made
+// nondecreasing (`from`: the boundary so far, advanced), so that groups never overlap.
+struct Groups : Shape {
+  __device__ __forceinline__ Groups(const SharedArgs& a, const GroupRow& r, int& from) {
+    int s = r.start, e = r.end;
+    if (__builtin_amdgcn_ballot_w64(e < s || s < from)) {   // (boundaries that fall)
+      s = max(max_scan(s), from);
+      e = max(s, e);
+      from = last_lane(max_scan(e));
+    } else {
+      from = last_lane(e);
+    }
+    static_cast<Shape&>(*this) = Shape(s, e, r.len, a.log2_group);
   }
 };
 
@@ -124,26 +129,56 @@ struct Teams {
   }
 };
 
-// Where the work and the slots of 64 prefixes of one kind begin: units (few) or workers
-// (team), and slots.  `work` and `slots` count those before, and are advanced.
+// Units with starts (few) or workers (team) of a prefix, and its slots (few: besides one for each worker).
+struct Amounts {
+  int work, slots;
+  __device__ __forceinline__ Amounts(const Shape& x, const SharedPlan& plan, int kind, int hkv)
+      : work(hkv * (x.units + 1)), slots(hkv) {
+    if (kind == kTeam) {
+      const Teams t(plan, x.units, hkv);
+      work = (plan.team_aligned ? hkv : 1) * t.cuts * x.tiles;
+      slots = (plan.team_aligned ? hkv * t.cuts : hkv + t.cuts) * x.wide;
+    }
+  }
+};
+
+// Where the work and the slots of 64 prefixes of one kind begin.  `work` and `slots`
+// count those before, and are advanced.
 struct Places {
   int base, end, slot;
   __device__ __forceinline__ Places(const Groups& x, const SharedPlan& plan, int kind, int hkv, int& work, int& slots) {
-    int w = hkv * x.units, n = hkv;   // few: a slot for each segment (and one for each worker)
-    if (kind == kTeam) {
-      const Teams t(plan, x.units, hkv);
-      w = (plan.team_aligned ? hkv : 1) * t.cuts * x.tiles;
-      n = (plan.team_aligned ? hkv * t.cuts : hkv + t.cuts) * x.wide;
-    }
+    const Amounts n(x, plan, kind, hkv);
     const bool mine = x.kind == kind;
-    const LaneSum sw(mine ? w : 0), sn(mine ? n : 0);
+    const LaneSum sw(mine ? n.work : 0), sn(mine ? n.slots : 0);
     base = work + sw.before;
-    end = mine ? base + w : base;
+    end = mine ? base + n.work : base;
     slot = slots + sn.before;
     work += sw.total;
     slots += sn.total;
   }
 };
+
+// One prefix and its place.
+struct Group : Shape {
+  int p, base, end, slot;
+  __device__ __forceinline__ Group() {}
+  __device__ __forceinline__ Group(const Groups& x, const Places& at, int c0, int l) {
+    p = c0 + l;
+    start = lane_value(x.start, l);
+    count = lane_value(x.count, l);
+    units = lane_value(x.units, l);
+    len = lane_value(x.len, l);
+    kind = lane_value(x.kind, l);
+    tiles = lane_value(x.tiles, l);
+    wide = lane_value(x.wide, l);
+    base = lane_value(at.base, l);
+    end = lane_value(at.end, l);
+    slot = lane_value(at.slot, l);
+  }
+};
+
+// A row's units in the flat space of its kind, for one KV head.
+__device__ __forceinline__ int work_of(int len) { return len > 0 ? units_of(len) + 1 : 0; }
 
 // 64 sequences, one a lane: their own tokens and where their units begin.
 struct SequenceSums {
@@ -157,7 +192,7 @@ struct Sequences {
   // (length: of sequence chunk + lane)
   __device__ __forceinline__ Sequences(const SharedArgs& a, SequenceSums& sums, int length) : len(length) {
     units = units_of(len);
-    const int n = a.num_kv_heads * units, incl = sum_scan(n);
+    const int n = a.num_kv_heads * work_of(len), incl = sum_scan(n);
     base = sums.units + incl - n;
     sums.chunk += 64;
     sums.units += last_lane(incl);
@@ -444,31 +479,34 @@ struct Worker {
 struct Describe {
   int4 units;   // off, head_off, units, run of the prefix (run 0: none)
   int4 slots;   // slot, head_slot, step, col
-  int4 own;     // off, units, run (0: none), 0
+  int4 own;     // off, units, run (0: none), 0; a head's segment is units + 1 further than the one before
 };
 
 // The prefix's part, for the sequences of chunk `chunk` (one a lane) that stand behind
-// the 64 prefixes x of one kind; slot0: that kind's first slot.
-__device__ __forceinline__ void describe_prefix(Describe& d, const SharedArgs& a, const SharedPlan& plan, const Groups& x,
-                                                const Places& at, int kind, int slot0, int chunk, int lane) {
+// prefix g; slot0: its kind's first slot.
+__device__ __forceinline__ void describe_prefix(Describe& d, const SharedArgs& a, const SharedPlan& plan, const Group& g, int slot0,
+                                                int chunk, int lane) {
   const int s = 64 * chunk + lane;
+  if (s < g.start || s >= g.start + g.count) return;
+  const int j = (s - g.start) << a.log2_group, slot = slot0 + g.slot;
+  if (g.kind == kFew) {
+    d.units = int4{g.base + 1, g.units + 1, g.units, plan.few_run};
+    d.slots = int4{slot, 1, 1, j};
+  } else {
+    const Teams t(plan, g.units, a.num_kv_heads);
+    d.units = int4{0, plan.team_aligned ? t.cuts * t.run : g.units, g.units, t.run};
+    d.slots = int4{slot + j / kPfCols, plan.team_aligned ? 0 : g.wide, g.wide, j & (kPfCols - 1)};
+  }
+}
+// Those of one kind among the 64 prefixes x whose groups reach into these sequences.
+__device__ __forceinline__ void describe_prefixes(Describe& d, const SharedArgs& a, const SharedPlan& plan, const Groups& x,
+                                                  const Places& at, int kind, int slot0, int chunk, int lane) {
   uint64_t some = __builtin_amdgcn_ballot_w64(x.kind == kind && x.start < 64 * (chunk + 1) && x.start + x.count > 64 * chunk);
 #pragma unroll 1
-  while (some) {   // the prefixes whose groups reach into these sequences
+  while (some) {
     const int l = __builtin_ctzll(some);
     some &= some - 1;
-    const int start = lane_value(x.start, l), units = lane_value(x.units, l), wide = lane_value(x.wide, l);
-    const int base = lane_value(at.base, l), slot = slot0 + lane_value(at.slot, l);
-    if (s < start || s >= start + lane_value(x.count, l)) continue;
-    const int j = (s - start) << a.log2_group;
-    if (kind == kFew) {
-      d.units = int4{base, units, units, plan.few_run};
-      d.slots = int4{slot, 1, 1, j};
-    } else {
-      const Teams t(plan, units, a.num_kv_heads);
-      d.units = int4{0, plan.team_aligned ? t.cuts * t.run : units, units, t.run};
-      d.slots = int4{slot + j / kPfCols, plan.team_aligned ? 0 : wide, wide, j & (kPfCols - 1)};
-    }
+    describe_prefix(d, a, plan, Group(x, at, 0, l), slot0, chunk, lane);
   }
 }
 // The sequences' own part.
@@ -479,42 +517,46 @@ __device__ __forceinline__ void describe_own(Describe& d, const SharedArgs& a, c
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
       const int t = c + 64 * u + lane;
-      before += units_of(t < 64 * chunk ? own_length(a, t) : 0);
+      before += work_of(t < 64 * chunk ? own_length(a, t) : 0);
     }
   }
   SequenceSums ss{64 * chunk, a.num_kv_heads * last_lane(sum_scan(before))};
   const Sequences y(a, ss, own_length(a, 64 * chunk + lane));
-  if (y.units > 0) d.own = int4{y.base, y.units, plan.own_run, 0};
+  if (y.units > 0) d.own = int4{y.base + 1, y.units, plan.own_run, 0};
 }
 
 // ---- the kernel ---------------------------------------------------------------
 
+// The launch's arguments, through an opaque pointer to them: a field is loaded where it
+// is used (a scalar load that hits the cache), not kept in scalar registers, of which
+// there are too few, from the kernel's start.
+__device__ __forceinline__ const SharedArgs& arguments() {
+  auto p = (const __attribute__((address_space(4))) SharedArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const SharedArgs*)p;
+}
+
 template <typename T, bool ELASTIC, bool F8>
-__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void shared_kernel(SharedArgs a) {
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void shared_kernel(SharedArgs) {
+  const SharedArgs& a = arguments();
   __shared__ __attribute__((aligned(16))) char ring[kLdsBytes];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hkv = a.num_kv_heads;
 
   // (the first 64 prefixes and sequences are read once and kept in LDS, a copy for every wave)
   int4* rows0 = reinterpret_cast<int4*>(ring + kLdsRing) + 64 * wave + lane;
-  int own_units, own_rows;   // (rows with tokens)
+  int own_work;   // units and starts of all sequences
   {
     const GroupRow r(a, 0, lane);
     const int len0 = own_length(a, lane);
     *rows0 = int4{r.start, r.end, r.len, len0};
-    own_units = units_of(len0);
-    own_rows = len0 > 0 ? 1 : 0;
+    own_work = work_of(len0);
   }
 #pragma unroll 1
   for (int c = 64; c < a.own.rows; c += 512) {   // (8 loads in flight)
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      const int n = units_of(own_length(a, c + 64 * u + lane));
-      own_units += n;
-      own_rows += n > 0 ? 1 : 0;
-    }
+    for (int u = 0; u < 8; ++u) own_work += work_of(own_length(a, c + 64 * u + lane));
   }
-  own_units = hkv * last_lane(sum_scan(own_units));
-  own_rows = last_lane(sum_scan(own_rows));
+  own_work = hkv * last_lane(sum_scan(own_work));
 
   // One loop scans the prefixes and works, so that the code of either is there once (a
   // launch starts with a cold instruction cache): pass 0 adds up the work of each kind
@@ -523,19 +565,38 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   SharedPlan plan{};
   int kind = kNone;              // of this worker (kNone: a wave for the sequences' own tokens)
   int id = 0, pos = 0, end = 0;  // its number in its kind (few, own: this wave's); its units (team: its number)
-  int few_units = 0, team_units = 0, team_tiles = 0, few_segments = 0, team_slot0 = 0;   // (the few's slots come first)
+  int few_work = 0, team_units = 0, team_tiles = 0, few_segments = 0, team_slot0 = 0;   // (the few's slots come first)
 #pragma unroll 1
   for (int pass = 0;; ++pass) {
-    struct {
-      int p, start, count, units, len, tiles, wide, base, slot, end;
-    } at{};
+    const SharedArgs& a = arguments();
+    Group at;
     bool found = pass > 0 && kind == kNone;
     const int chunk = gridDim.x - 1 - blockIdx.x;   // the last workgroups describe 64 sequences each
     const bool describes = pass == 1 && wave == 0 && 64 * chunk < a.own.rows;
     Describe d{int4{0, 0, 0, 0}, int4{0, 0, 1, 0}, int4{0, 0, 0, 0}};
     int from = 0, work = 0, slots = 0, other_work = 0, other_slots = 0;
+    const bool one = a.prefix.rows == 1;   // (in scalars, without a scan: a third of the time)
+    if (one) {
+      const int4 v = *rows0;
+      const int start = lane_value(v.x, 0);
+      static_cast<Shape&>(at) = Shape(start, max(start, lane_value(v.y, 0)), lane_value(v.z, 0), a.log2_group);
+      at.p = at.base = at.slot = 0;
+      if (pass == 0) {
+        if (at.kind == kFew) {
+          few_work = hkv * (at.units + 1);
+          few_segments = hkv;
+        } else if (at.kind == kTeam) {
+          team_tiles = at.tiles;
+          team_units = hkv * at.tiles * at.units;
+        }
+      } else if (at.kind != kNone) {
+        at.end = Amounts(at, plan, at.kind, hkv).work;
+        found = found || (at.kind == kind && pos < at.end);
+        if (describes) describe_prefix(d, a, plan, at, at.kind == kTeam ? team_slot0 : 0, chunk, lane);
+      }
+    }
 #pragma unroll 1
-    for (int c0 = 0; c0 < a.prefix.rows && (pass < 2 || !found); c0 += 64) {
+    for (int c0 = one ? 1 : 0; c0 < a.prefix.rows && (pass < 2 || !found); c0 += 64) {
       GroupRow r(0, 0, 0);
       if (c0 == 0) {
         const int4 v = *rows0;
@@ -546,7 +607,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
       const Groups x(a, r, from);
       if (pass == 0) {
         const bool team = x.kind == kTeam;
-        few_units += LaneSum(x.kind == kFew ? hkv * x.units : 0).total;
+        few_work += LaneSum(x.kind == kFew ? hkv * (x.units + 1) : 0).total;
         few_segments += hkv * __builtin_popcountll(__builtin_amdgcn_ballot_w64(x.kind == kFew));
         team_units += LaneSum(team ? hkv * x.tiles * x.units : 0).total;
         team_tiles += LaneSum(team ? x.tiles : 0).total;
@@ -555,28 +616,18 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
       if (describes) {
         const int other = kind == kTeam ? kFew : kTeam;   // (own workers: both kinds, one here and one below)
         const Places y(x, plan, other, hkv, other_work, other_slots);
-        describe_prefix(d, a, plan, x, y, other, other == kTeam ? team_slot0 : 0, chunk, lane);
+        describe_prefixes(d, a, plan, x, y, other, other == kTeam ? team_slot0 : 0, chunk, lane);
       }
       const int mine = kind == kNone ? kFew : kind;
       const Places y(x, plan, mine, hkv, work, slots);
-      if (describes) describe_prefix(d, a, plan, x, y, mine, mine == kTeam ? team_slot0 : 0, chunk, lane);
+      if (describes) describe_prefixes(d, a, plan, x, y, mine, mine == kTeam ? team_slot0 : 0, chunk, lane);
       const uint64_t hit = __builtin_amdgcn_ballot_w64(x.kind == mine && y.base <= pos && pos < y.end);
       if (found || !hit) continue;
       found = true;
-      const int l = __builtin_ctzll(hit);
-      at.p = c0 + l;
-      at.start = lane_value(x.start, l);
-      at.count = lane_value(x.count, l);
-      at.units = lane_value(x.units, l);
-      at.len = lane_value(x.len, l);
-      at.tiles = lane_value(x.tiles, l);
-      at.wide = lane_value(x.wide, l);
-      at.base = lane_value(y.base, l);
-      at.slot = lane_value(y.slot, l);
-      at.end = lane_value(y.end, l);
+      at = Group(x, y, c0, __builtin_ctzll(hit));
     }
     if (pass == 0) {
-      plan = divide_work(SharedWork{team_units, team_tiles, hkv * team_tiles, few_units, few_segments, own_units, hkv * own_rows},
+      plan = divide_work(SharedWork{team_units, team_tiles, hkv * team_tiles, few_work, own_work},
                          (int)gridDim.x, a.min_units, F8);
       team_slot0 = few_segments + kWaves * plan.few_workers;
       id = blockIdx.x;
@@ -594,7 +645,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         id = id * kWaves + wave;
         const int run = kind == kFew ? plan.few_run : plan.own_run;
         pos = id * run;
-        end = min(kind == kFew ? few_units : own_units, pos + run);
+        end = min(kind == kFew ? few_work : own_work, pos + run);
       }
       continue;
     }
@@ -605,6 +656,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     if (!found || pos >= end) return;
 
     if (kind == kTeam) {
+      const SharedArgs& a = arguments();
       const Teams t(plan, at.units, hkv);
       const int team = (pos - at.base) / at.tiles, tile = (pos - at.base) - team * at.tiles;
       const int k = team / t.cuts, first = tile * kTileCols;   // span; first column
@@ -621,7 +673,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         pc.seq0 = at.start + (first >> a.log2_group);
         pc.columns = min((at.count << a.log2_group) - first, kTileCols);
         pc.slot = team_slot0 + at.slot + (team + (plan.team_aligned ? 0 : pc.kvh)) * at.wide + kWaves * tile;
-        Worker<T, ELASTIC, F8>(a, ring, wave, fresh(lane)).tile(pc);
+        Worker<T, ELASTIC, F8>(arguments(), ring, wave, fresh(lane)).tile(pc);
         u += pc.u1 - pc.u0;
       }
       pos += plan.team_workers;   // (more of the prefixes' tiles than workers: another round)
@@ -642,7 +694,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         seqs = ss.chunk;
         if (seqs > 0) lens = own_length(a, seqs + lane);
         const Sequences y(a, ss, lens);
-        hit = __builtin_amdgcn_ballot_w64(y.base <= u && u < y.base + hkv * y.units);
+        hit = __builtin_amdgcn_ballot_w64(y.base <= u && u < y.base + hkv * work_of(lens));
         if (!hit) continue;
         lane_at = __builtin_ctzll(hit);
         at.base = lane_value(y.base, lane_at);
@@ -670,15 +722,18 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         at.p = at.start = seqs + lane_at;
         at.len = lane_value(lens, lane_at);
         at.units = units_of(at.len);
-        at.end = at.base + hkv * at.units;
+        at.end = at.base + hkv * (at.units + 1);
         at.count = 1;
         at.slot = at.p * hkv;
       }
-      const int off = u - at.base;
       x.row = at.p;
       x.len = at.len;
-      x.kvh = off / at.units;
-      x.u0 = off - x.kvh * at.units;
+      x.kvh = (u - at.base) / (at.units + 1);
+      x.u0 = u - at.base - x.kvh * (at.units + 1) - 1;
+      if (x.u0 < 0) {       // the segment's start
+        x.u0 = 0;
+        if (++u >= u_end) return false;
+      }
       x.u1 = min(at.units, x.u0 + min(64, u_end - u));
       x.seq0 = at.start;
       x.columns = at.count << a.log2_group;
@@ -686,7 +741,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
       u += x.u1 - x.u0;
       return true;
     };
-    Worker<T, ELASTIC, F8>(a, ring, wave, fresh(lane)).stream(few ? a.prefix : a.own, next, few ? a.o_wide : a.o_own, few ? a.ml_wide : a.ml_own,
+    Worker<T, ELASTIC, F8>(arguments(), ring, wave, fresh(lane)).stream(few ? a.prefix : a.own, next, few ? a.o_wide : a.o_own, few ? a.ml_wide : a.ml_own,
                   few ? a.wide_slots : a.own_slots, few ? kPfCols : 1 << a.log2_group);
     if (!few) return;
     pos = u_end;
@@ -748,35 +803,69 @@ struct Pieces {
   }
 };
 
+// `ways` (1, 2, 4 or 8) waves divide a column's pieces between them and join theirs
+// through LDS; a workgroup then has 8 / ways waves' chunks, and grid z is ways.
 template <typename T>
 __global__ __launch_bounds__(64 * kMergeWaves) void shared_merge_kernel(SharedArgs a) {
+  __shared__ float parts[kMergeWaves][10][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kvh = blockIdx.y;
-  const int c = blockIdx.x * kPfCols + (lane & 31), chunk = 4 * wave + (lane >> 5);
+  const int kvh = blockIdx.y, ways = gridDim.z, way = wave & (ways - 1);
+  const int c = blockIdx.x * kPfCols + (lane & 31);
+  const int chunk = 4 * ((wave + kMergeWaves * blockIdx.z) / ways) + (lane >> 5);
   const int s = c >> a.log2_group, head = c & ((1 << a.log2_group) - 1);
-  if (s >= a.own.rows) return;
-  const Describe d = reinterpret_cast<const Describe*>(a.plan)[s];
-  int wide_n = 0, wide_slot = 0, own_n = 0, own_slot = 0;
-  if (d.units.w > 0) {
-    const int off = d.units.x + kvh * d.units.y, w0 = off / d.units.w;
-    wide_n = (off + d.units.z - 1) / d.units.w - w0 + 1;
-    wide_slot = d.slots.x + kvh * d.slots.y + w0 * d.slots.z;
+  const bool ok = s < a.own.rows;
+  int wide_n = 0, wide_slot = 0, own_n = 0, own_slot = 0, step = 1, col = 0;
+  if (ok) {
+    const Describe d = reinterpret_cast<const Describe*>(a.plan)[s];
+    if (d.units.w > 0) {
+      const int off = d.units.x + kvh * d.units.y, w0 = off / d.units.w;
+      wide_n = (off + d.units.z - 1) / d.units.w - w0 + 1;
+      wide_slot = d.slots.x + kvh * d.slots.y + w0 * d.slots.z;
+      step = d.slots.z;
+      col = d.slots.w + head;
+    }
+    if (d.own.z > 0) {
+      const int off = d.own.x + kvh * (d.own.y + 1), w0 = off / d.own.z;
+      own_n = (off + d.own.y - 1) / d.own.z - w0 + 1;
+      own_slot = s * a.num_kv_heads + kvh + w0;
+    }
   }
-  if (d.own.z > 0) {
-    const int off = d.own.x + kvh * d.own.y, w0 = off / d.own.z;
-    own_n = (off + d.own.y - 1) / d.own.z - w0 + 1;
-    own_slot = s * a.num_kv_heads + kvh + w0;
-  }
+  const int all_n = wide_n + own_n;
+  // this way's pieces: every `ways`-th from `way` on
+  wide_slot += way * step;
+  own_slot += way;
+  wide_n = (wide_n - way + ways - 1) / ways;
+  own_n = (own_n - way + ways - 1) / ways;
   Joined j;
   constexpr int kWide = 8, kOwn = 4;
 #pragma unroll 1
   for (int w0 = 0, o0 = 0; __builtin_amdgcn_ballot_w64(w0 < wide_n || o0 < own_n); w0 += kWide, o0 += kOwn) {
-    const Pieces<kWide> w(a.o_wide, a.ml_wide, w0, wide_n, wide_slot, d.slots.z, kPfCols, d.slots.w + head, a.wide_slots, chunk);
-    const Pieces<kOwn> o(a.o_own, a.ml_own, o0, own_n, own_slot, 1, 1 << a.log2_group, head, a.own_slots, chunk);
+    const Pieces<kWide> w(a.o_wide, a.ml_wide, w0, wide_n, wide_slot, step * ways, kPfCols, col, a.wide_slots, chunk);
+    const Pieces<kOwn> o(a.o_own, a.ml_own, o0, own_n, own_slot, ways, 1 << a.log2_group, head, a.own_slots, chunk);
     w.join(j);
     o.join(j);
   }
-  const float inv = wide_n + own_n > 0 ? 1.0f / j.l : 0.f;   // (a sequence without any token: zeros)
+  if (ways > 1) {
+    if (way > 0) {
+      parts[wave][0][lane] = j.m;
+      parts[wave][1][lane] = j.l;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) parts[wave][2 + i][lane] = j.o[i >> 2][i & 3];
+    }
+    __syncthreads();
+    if (way > 0) return;
+#pragma unroll 1
+    for (int w = wave + 1; w < wave + ways; ++w) {
+      const float m = parts[w][0][lane], top = fmaxf(j.m, m), base = finite_or_zero(top);
+      const float f = fast_exp2(j.m - base), e = fast_exp2(m - base);
+      j.l = j.l * f + parts[w][1][lane] * e;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) j.o[i >> 2][i & 3] = j.o[i >> 2][i & 3] * f + parts[w][2 + i][lane] * e;
+      j.m = top;
+    }
+  }
+  if (!ok) return;
+  const float inv = all_n > 0 ? 1.0f / j.l : 0.f;   // (a sequence without any token: zeros)
   const size_t row = ((size_t)s * a.num_q_heads + (kvh << a.log2_group) + head) * kHeadDim;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -793,7 +882,7 @@ hipError_t launch_typed(const SharedArgs& a, bool elastic, hipStream_t st) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int columns = a.own.rows << a.log2_group;
-  hipLaunchKernelGGL((shared_merge_kernel<T>), dim3((columns + kPfCols - 1) / kPfCols, a.num_kv_heads),
+  hipLaunchKernelGGL((shared_merge_kernel<T>), dim3((columns + kPfCols - 1) / kPfCols, a.num_kv_heads, a.merge_ways),
                      dim3(64 * kMergeWaves), 0, st, a);
   return hipGetLastError();
 }

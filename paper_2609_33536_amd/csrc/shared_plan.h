@@ -31,14 +31,15 @@ struct SharedArgs {
   int32_t num_kv_heads, num_q_heads, log2_group, out_fp32;
   int32_t grid;              // workgroups, at least 4 (one for each kind of work)
   int32_t min_units;         // fewest units of a prefix that a worker takes
+  int32_t merge_ways;        // waves that divide a column's pieces in the merge: 1, 2, 4 or 8
   float scale_log2;
 };
 
 constexpr int kMaxSharedGrid = 512;
 
-// Units and segments of each kind; a team's count once for each of its tiles.
+// Units (few, own: and segments) of each kind; a team's count once for each of its tiles.
 struct SharedWork {
-  int team_units, team_tiles, team_segments, few_units, few_segments, own_units, own_segments;
+  int team_units, team_tiles, team_segments, few_work, own_work;
 };
 
 // Workgroups of each kind, and the units that one of their waves takes (few, own), or
@@ -51,25 +52,26 @@ struct SharedPlan {
 // Divides `grid` workgroups (at least 4) over the kinds by their units and
 // segments, weighted by what these cost a workgroup: a tile's unit is matrix work
 // of 4 waves, the others' are bytes from HBM (half as many for 8-bit pools); a
-// segment costs its start (table, queries, first loads) and its partials.
+// segment costs its start (table, queries, first loads) and its partials, 5 units of
+// a tile and one of a wave's stream.
 __host__ __device__ inline SharedPlan divide_work(const SharedWork& n, int grid, int min_units, bool bytes8) {
   const float stream = bytes8 ? 2.f : 3.f;
   const float team = 4.f * n.team_units + 20.f * n.team_segments;
-  const float few = stream * n.few_units + 3.f * n.few_segments, own = stream * n.own_units + 3.f * n.own_segments;
+  const float few = stream * n.few_work, own = stream * n.own_work;
   const float share = grid / fmaxf(1.f, team + few + own);
   int t = (int)(share * team), f = (int)(share * few), o = (int)(share * own);
   if (n.team_units > 0 && t == 0) t = 1;
-  if (n.few_units > 0 && f == 0) f = 1;
-  if (n.own_units > 0 && o == 0) o = 1;
+  if (n.few_work > 0 && f == 0) f = 1;
+  if (n.own_work > 0 && o == 0) o = 1;
   // (what rounding left over or took too much)
   const int rest = grid - t - f - o;
   if (t >= f && t >= o) t += rest;
   else if (f >= o) f += rest;
   else o += rest;
   SharedPlan p{t, f, o, 1, 0, 1, 1};
-  if (n.few_units > 0) p.few_run = (n.few_units + 4 * f - 1) / (4 * f);
+  if (n.few_work > 0) p.few_run = (n.few_work + 4 * f - 1) / (4 * f);
   if (p.few_run < min_units) p.few_run = min_units;
-  if (n.own_units > 0) p.own_run = (n.own_units + 4 * o - 1) / (4 * o);
+  if (n.own_work > 0) p.own_run = (n.own_work + 4 * o - 1) / (4 * o);
   if (n.team_units > 0) {
     // every prefix (or segment) rounds its number of teams up, which adds at most its tiles
     const int half = (t + 1) / 2, free = t - n.team_tiles > half ? t - n.team_tiles : half;

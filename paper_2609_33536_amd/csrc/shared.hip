@@ -11,12 +11,13 @@
 //
 // One launch works on three kinds of segments (a segment: one KV head of a prefix, or of
 // a sequence's own tokens), each kind on workgroups of its own:
-//   team   a prefix with more than 32 query columns (sequence of the group, head of the
-//          KV head's G): a team of workgroups, one for each tile of 128 columns, takes a
-//          run of a segment's units, so that all of the team read the same K and V at
-//          the same time, on one XCD.  In a tile 4 waves x 32 columns share every unit,
-//          pipelined as in prefill.hip;
-//   few    a prefix with at most 32 columns: a wave streams its units alone;
+//   team   a prefix's query columns (sequence of the group, head of the KV head's G) in
+//          tiles of 128: a team of workgroups, one for each tile, takes a run of a
+//          segment's units, so that all of the team read the same K and V at the same
+//          time, on one XCD.  In a tile 4 waves x 32 columns share every unit, pipelined
+//          as in prefill.hip;
+//   few    a prefix's columns if they are at most 32, or at most 32 left over by the
+//          tiles: a wave streams the units alone;
 //   own    a sequence's own tokens, G columns: likewise.
 // The workgroups are divided between the kinds by the work that each has.  The units of
 // few and own are one flat space each, in which a segment's start counts as a unit; a
@@ -88,19 +89,26 @@ struct GroupRow {
   }
 };
 
-// What follows from a prefix's sequences and length.
+// What follows from a prefix's sequences and length.  Its columns go to tiles of 128;
+// up to 32 of them, or up to 32 left over by the tiles, to a wave's stream (the last
+// sequences' columns: a tile's unit costs the same for one column as for 128, and
+// more than a stream's).
 struct Shape {
-  int start, count, units, len, kind;
+  int start, count, units, len;            // (units: 0 without any sequence)
   int tiles, wide;                         // tiles of 128 and groups of 32 columns
+  int rest;                                // columns of the stream
   __device__ __forceinline__ Shape() {}
   __device__ __forceinline__ Shape(int start_, int end, int len_, int log2_group) : start(start_), len(len_) {
     count = len > 0 ? end - start : 0;
-    const int columns = count << log2_group;
     units = count > 0 ? units_of(len) : 0;
-    tiles = (columns + kTileCols - 1) / kTileCols;
-    wide = (columns + kPfCols - 1) / kPfCols;
-    kind = units == 0 ? kNone : (columns <= kPfCols ? kFew : kTeam);
+    const int columns = count << log2_group;
+    rest = columns % kTileCols <= kPfCols ? columns % kTileCols : 0;
+    tiles = (columns - rest + kTileCols - 1) / kTileCols;
+    wide = (columns - rest + kPfCols - 1) / kPfCols;
   }
+  __device__ __forceinline__ bool has(int kind) const { return kind == kTeam ? tiles > 0 : rest > 0; }
+  // the first sequence of the stream's columns
+  __device__ __forceinline__ int rest_start(int log2_group) const { return start + count - (rest >> log2_group); }
 };
 
 // Of 64 prefixes.  The group boundaries are clamped into the batch and made
@@ -148,7 +156,7 @@ struct Places {
   int base, end, slot;
   __device__ __forceinline__ Places(const Groups& x, const SharedPlan& plan, int kind, int hkv, int& work, int& slots) {
     const Amounts n(x, plan, kind, hkv);
-    const bool mine = x.kind == kind;
+    const bool mine = x.has(kind);
     const LaneSum sw(mine ? n.work : 0), sn(mine ? n.slots : 0);
     base = work + sw.before;
     end = mine ? base + n.work : base;
@@ -168,7 +176,7 @@ struct Group : Shape {
     count = lane_value(x.count, l);
     units = lane_value(x.units, l);
     len = lane_value(x.len, l);
-    kind = lane_value(x.kind, l);
+    rest = lane_value(x.rest, l);
     tiles = lane_value(x.tiles, l);
     wide = lane_value(x.wide, l);
     base = lane_value(at.base, l);
@@ -483,13 +491,14 @@ struct Describe {
 };
 
 // The prefix's part, for the sequences of chunk `chunk` (one a lane) that stand behind
-// prefix g; slot0: its kind's first slot.
-__device__ __forceinline__ void describe_prefix(Describe& d, const SharedArgs& a, const SharedPlan& plan, const Group& g, int slot0,
-                                                int chunk, int lane) {
-  const int s = 64 * chunk + lane;
-  if (s < g.start || s >= g.start + g.count) return;
-  const int j = (s - g.start) << a.log2_group, slot = slot0 + g.slot;
-  if (g.kind == kFew) {
+// prefix g in its columns of one kind; slot0: that kind's first slot.
+__device__ __forceinline__ void describe_prefix(Describe& d, const SharedArgs& a, const SharedPlan& plan, const Group& g, int kind,
+                                                int slot0, int chunk, int lane) {
+  const int s = 64 * chunk + lane, rest = g.rest_start(a.log2_group);
+  const int first = kind == kFew ? rest : g.start;
+  if (s < first || s >= (kind == kFew ? g.start + g.count : rest)) return;
+  const int j = (s - first) << a.log2_group, slot = slot0 + g.slot;
+  if (kind == kFew) {
     d.units = int4{g.base + 1, g.units + 1, g.units, plan.few_run};
     d.slots = int4{slot, 1, 1, j};
   } else {
@@ -501,12 +510,12 @@ __device__ __forceinline__ void describe_prefix(Describe& d, const SharedArgs& a
 // Those of one kind among the 64 prefixes x whose groups reach into these sequences.
 __device__ __forceinline__ void describe_prefixes(Describe& d, const SharedArgs& a, const SharedPlan& plan, const Groups& x,
                                                   const Places& at, int kind, int slot0, int chunk, int lane) {
-  uint64_t some = __builtin_amdgcn_ballot_w64(x.kind == kind && x.start < 64 * (chunk + 1) && x.start + x.count > 64 * chunk);
+  uint64_t some = __builtin_amdgcn_ballot_w64(x.has(kind) && x.start < 64 * (chunk + 1) && x.start + x.count > 64 * chunk);
 #pragma unroll 1
   while (some) {
     const int l = __builtin_ctzll(some);
     some &= some - 1;
-    describe_prefix(d, a, plan, Group(x, at, 0, l), slot0, chunk, lane);
+    describe_prefix(d, a, plan, Group(x, at, 0, l), kind, slot0, chunk, lane);
   }
 }
 // The sequences' own part.
@@ -582,17 +591,19 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
       static_cast<Shape&>(at) = Shape(start, max(start, lane_value(v.y, 0)), lane_value(v.z, 0), a.log2_group);
       at.p = at.base = at.slot = 0;
       if (pass == 0) {
-        if (at.kind == kFew) {
-          few_work = hkv * (at.units + 1);
-          few_segments = hkv;
-        } else if (at.kind == kTeam) {
-          team_tiles = at.tiles;
-          team_units = hkv * at.tiles * at.units;
+        few_work = at.has(kFew) ? hkv * (at.units + 1) : 0;
+        few_segments = at.has(kFew) ? hkv : 0;
+        team_tiles = at.tiles;
+        team_units = hkv * at.tiles * at.units;
+      } else {
+        if (kind != kNone && at.has(kind)) {
+          at.end = Amounts(at, plan, kind, hkv).work;
+          found = pos < at.end;
         }
-      } else if (at.kind != kNone) {
-        at.end = Amounts(at, plan, at.kind, hkv).work;
-        found = found || (at.kind == kind && pos < at.end);
-        if (describes) describe_prefix(d, a, plan, at, at.kind == kTeam ? team_slot0 : 0, chunk, lane);
+        if (describes) {
+          if (at.has(kTeam)) describe_prefix(d, a, plan, at, kTeam, team_slot0, chunk, lane);
+          if (at.has(kFew)) describe_prefix(d, a, plan, at, kFew, 0, chunk, lane);
+        }
       }
     }
 #pragma unroll 1
@@ -606,11 +617,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
       }
       const Groups x(a, r, from);
       if (pass == 0) {
-        const bool team = x.kind == kTeam;
-        few_work += LaneSum(x.kind == kFew ? hkv * (x.units + 1) : 0).total;
-        few_segments += hkv * __builtin_popcountll(__builtin_amdgcn_ballot_w64(x.kind == kFew));
-        team_units += LaneSum(team ? hkv * x.tiles * x.units : 0).total;
-        team_tiles += LaneSum(team ? x.tiles : 0).total;
+        few_work += LaneSum(x.has(kFew) ? hkv * (x.units + 1) : 0).total;
+        few_segments += hkv * __builtin_popcountll(__builtin_amdgcn_ballot_w64(x.has(kFew)));
+        team_units += LaneSum(hkv * x.tiles * x.units).total;
+        team_tiles += LaneSum(x.tiles).total;
         continue;
       }
       if (describes) {
@@ -621,7 +631,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
       const int mine = kind == kNone ? kFew : kind;
       const Places y(x, plan, mine, hkv, work, slots);
       if (describes) describe_prefixes(d, a, plan, x, y, mine, mine == kTeam ? team_slot0 : 0, chunk, lane);
-      const uint64_t hit = __builtin_amdgcn_ballot_w64(x.kind == mine && y.base <= pos && pos < y.end);
+      const uint64_t hit = __builtin_amdgcn_ballot_w64(x.has(mine) && y.base <= pos && pos < y.end);
       if (found || !hit) continue;
       found = true;
       at = Group(x, y, c0, __builtin_ctzll(hit));
@@ -671,7 +681,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         pc.u0 = u - pc.kvh * at.units;
         pc.u1 = min(at.units, pc.u0 + (u_end - u));
         pc.seq0 = at.start + (first >> a.log2_group);
-        pc.columns = min((at.count << a.log2_group) - first, kTileCols);
+        pc.columns = min((at.count << a.log2_group) - at.rest - first, kTileCols);
         pc.slot = team_slot0 + at.slot + (team + (plan.team_aligned ? 0 : pc.kvh)) * at.wide + kWaves * tile;
         Worker<T, ELASTIC, F8>(arguments(), ring, wave, fresh(lane)).tile(pc);
         u += pc.u1 - pc.u0;
@@ -723,7 +733,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         at.len = lane_value(lens, lane_at);
         at.units = units_of(at.len);
         at.end = at.base + hkv * (at.units + 1);
-        at.count = 1;
+        at.rest = 1 << a.log2_group;
         at.slot = at.p * hkv;
       }
       x.row = at.p;
@@ -735,8 +745,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         if (++u >= u_end) return false;
       }
       x.u1 = min(at.units, x.u0 + min(64, u_end - u));
-      x.seq0 = at.start;
-      x.columns = at.count << a.log2_group;
+      x.seq0 = few ? at.rest_start(a.log2_group) : at.start;
+      x.columns = at.rest;
       x.slot = at.slot + x.kvh + id;
       u += x.u1 - x.u0;
       return true;

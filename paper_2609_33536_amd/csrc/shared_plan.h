@@ -55,7 +55,7 @@ struct SharedPlan {
 // segment costs its start (table, queries, first loads) and its partials, 5 units of
 // a tile and one of a wave's stream.
 __host__ __device__ inline SharedPlan divide_work(const SharedWork& n, int grid, int min_units, bool bytes8) {
-  const float stream = bytes8 ? 2.f : 3.f;
+  const float stream = bytes8 ? 1.75f : 2.5f;
   const float team = 4.f * n.team_units + 20.f * n.team_segments;
   const float few = stream * n.few_work, own = stream * n.own_work;
   const float share = grid / fmaxf(1.f, team + few + own);

@@ -6,12 +6,13 @@
 // Angles of far positions need more than a float's 24 bits (at t = 10^6 a float
 // product is off by up to 0.03 rad), so theta_i comes as a fixed-point fraction of a
 // turn, T_i = theta_i / (2 pi) 2^64: t T_i mod 2^64 is the exact phase of T_i's
-// multiple, its top 32 bits keep 2^-32 of a turn, and full turns fall away without
-// a division.
+// multiple, and full turns fall away without a division.
 //
 // 8 lanes hold a head's 128 elements, lane c the pairs 8c .. 8c + 7 (half layout:
 // elements 8c.. and rotary_dim / 2 + 8c..; pair layout: 16c .. 16c + 15), so that a
 // lane's cosines and sines serve every head that its wave turns.
+#include <algorithm>
+
 #include "common.h"
 #include "rope.h"
 
@@ -20,15 +21,24 @@ namespace {
 
 constexpr int kWaves = 4;
 
-// cos and sin of 2 pi p 2^-32: the nearest quarter turn taken off exactly, then the
-// Taylor polynomials on [-pi/4, pi/4] (to x^10 and x^9: truncated below 2e-9).
-__device__ __forceinline__ void cos_sin(uint32_t p, float& c, float& s) {
-  const uint32_t quarter = (p + 0x20000000u) >> 30;
-  const int32_t rest = (int32_t)(p - (quarter << 30));
-  const float x = (float)rest * 1.46291807926715968e-9f;   // 2 pi / 2^32
+// cos and sin of 2 pi p 2^-64, to about half a unit in the last place: the nearest
+// quarter turn taken off exactly, the rest as x + e (a product and what it rounded away),
+// then the Taylor polynomials on [-pi/4, pi/4] (to x^10 and x^9: truncated below 2e-9),
+// their small terms added to x and to 1 - x^2 / 2 at the end.
+__device__ __forceinline__ void cos_sin(uint64_t p, float& c, float& s) {
+  constexpr double kUnit = 1.46291807926715968e-9;   // 2 pi / 2^32
+  constexpr float kHigh = (float)kUnit, kLow = (float)(kUnit - (double)kHigh);
+  const uint32_t quarter = ((uint32_t)(p >> 32) + 0x20000000u) >> 30;
+  const int32_t rest = (int32_t)((uint32_t)(p >> 32) - (quarter << 30));   // (|rest| <= 2^29)
+  const float r = (float)rest, below = (float)(rest - (int32_t)r) + (float)(uint32_t)p * 0x1p-32f;
+  const float x = r * kHigh;
+  const float e = fmaf(r, kHigh, -x) + fmaf(r, kLow, below * kHigh);
   const float z = x * x;
-  const float sn = x + x * z * (-1.0f / 6 + z * (1.0f / 120 + z * (-1.0f / 5040 + z * (1.0f / 362880))));
-  const float cs = 1.0f + z * (-0.5f + z * (1.0f / 24 + z * (-1.0f / 720 + z * (1.0f / 40320 + z * (-1.0f / 3628800)))));
+  const float odd = x * z * (-1.0f / 6 + z * (1.0f / 120 + z * (-1.0f / 5040 + z * (1.0f / 362880))));
+  const float even = z * z * (1.0f / 24 + z * (-1.0f / 720 + z * (1.0f / 40320 + z * (-1.0f / 3628800))));
+  const float half = 0.5f * z, top = 1.0f - half;
+  const float sn = x + fmaf(e, top, odd);
+  const float cs = top + (((1.0f - top) - half) + (even - fmaf(x, e, 0.5f * fmaf(x, x, -z))));
   const bool swap = quarter & 1;
   c = swap ? sn : cs;
   s = swap ? cs : sn;
@@ -67,41 +77,51 @@ __device__ __forceinline__ void floats8(u32x4 w, float (&x)[8]) {
 
 template <typename T, bool F8>
 __global__ __launch_bounds__(64 * kWaves) void rope_kernel(RopeArgs a) {
-  const int lane = threadIdx.x & 63, c = lane & 7;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 7;
   const int rows = a.num_q_heads + 2 * a.num_kv_heads;   // rows of a token: query heads, key heads, value heads
-  const int parts = (rows + a.rows_per_wave - 1) / a.rows_per_wave;
-  const int64_t item = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
-  if (item >= (int64_t)a.n * parts) return;
-  const int token = (int)(item / parts), part = (int)(item % parts);
-  const int row_end = min(rows, (part + 1) * a.rows_per_wave);
+  const unsigned parts = (unsigned)(rows + a.rows_per_wave - 1) / a.rows_per_wave, item = blockIdx.x * kWaves + wave;
+  const int token = item / parts, row0 = (item - token * parts) * a.rows_per_wave;
+  if (token >= a.n) return;
+  const int row_end = min(rows, row0 + a.rows_per_wave);
 
   const int slot = a.slots[token];
   const int64_t position = a.positions[token];
-  const bool in_pool = slot >= 0 && slot / kPage < a.num_blocks;   // (outside the pool: the cache is left as it is)
   const int turned = a.rotary_dim / 16;                            // lanes whose pairs turn
+  // this lane's two 8-element chunks of a head
+  const int chunk0 = a.pairs ? 2 * c : (c < turned ? c : 2 * turned + 2 * (c - turned));
+  const int chunk1 = a.pairs ? 2 * c + 1 : (c < turned ? turned + c : chunk0 + 1);
+  const int values0 = a.num_q_heads + a.num_kv_heads;              // the first value head
+  auto load = [&](int r, u32x4& w0, u32x4& w1) {
+    const uint16_t* src = r < a.num_q_heads ? a.q + token * a.q_stride + (size_t)r * kHeadDim
+                          : r < values0     ? a.k + token * a.k_stride + (size_t)(r - a.num_q_heads) * kHeadDim
+                                            : a.v + token * a.v_stride + (size_t)(r - values0) * kHeadDim;
+    w0 = *reinterpret_cast<const u32x4*>(src + 8 * chunk0);
+    w1 = *reinterpret_cast<const u32x4*>(src + 8 * chunk1);
+  };
+  // (the first row's values are on their way while the angles are worked out, the next row's while one is turned)
+  int r = row0 + (lane >> 3);
+  u32x4 next0{0u, 0u, 0u, 0u}, next1{0u, 0u, 0u, 0u};
+  if (r < row_end) load(r, next0, next1);
+
+  const bool in_pool = slot >= 0 && slot / kPage < a.num_blocks;   // (outside the pool: the cache is left as it is)
   float cs[8], sn[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     cs[i] = 1.0f;
     sn[i] = 0.0f;
     if (c < turned) {
-      const uint64_t phase = (uint64_t)position * a.turns[8 * c + i];
-      cos_sin((uint32_t)((phase + 0x80000000ull) >> 32), cs[i], sn[i]);
+      cos_sin((uint64_t)position * a.turns[8 * c + i], cs[i], sn[i]);
       cs[i] *= a.magnitude;
       sn[i] *= a.magnitude;
     }
   }
-  // this lane's two 8-element chunks of a head
-  const int chunk0 = a.pairs ? 2 * c : (c < turned ? c : 2 * turned + 2 * (c - turned));
-  const int chunk1 = a.pairs ? 2 * c + 1 : (c < turned ? turned + c : chunk0 + 1);
 
-  for (int r = part * a.rows_per_wave + (lane >> 3); r < row_end; r += 8) {
-    const int head = r < a.num_q_heads ? r : (r - a.num_q_heads) % a.num_kv_heads;
-    const int kind = r < a.num_q_heads ? 0 : (r < a.num_q_heads + a.num_kv_heads ? 1 : 2);   // query, key, value
+#pragma unroll 1
+  for (; r < row_end; r += 8) {
+    u32x4 w0 = next0, w1 = next1;
+    if (r + 8 < row_end) load(r + 8, next0, next1);
+    const int kind = r < a.num_q_heads ? 0 : (r < values0 ? 1 : 2);   // query, key, value
     if (kind != 0 && !in_pool) continue;
-    const uint16_t* src = (kind == 0 ? a.q + token * a.q_stride : (kind == 1 ? a.k + token * a.k_stride : a.v + token * a.v_stride)) +
-                          (size_t)head * kHeadDim;
-    u32x4 w0 = *reinterpret_cast<const u32x4*>(src + 8 * chunk0), w1 = *reinterpret_cast<const u32x4*>(src + 8 * chunk1);
     float x[8], y[8];
     if (kind != 2 && c < turned) {
       floats8<T>(w0, x);
@@ -130,10 +150,11 @@ __global__ __launch_bounds__(64 * kWaves) void rope_kernel(RopeArgs a) {
       floats8<T>(w1, y);
     }
     if (kind == 0) {
-      uint16_t* dst = a.q_out + token * a.out_stride + (size_t)head * kHeadDim;
+      uint16_t* dst = a.q_out + token * a.out_stride + (size_t)r * kHeadDim;
       *reinterpret_cast<u32x4*>(dst + 8 * chunk0) = w0;
       *reinterpret_cast<u32x4*>(dst + 8 * chunk1) = w1;
     } else {
+      const int head = r - (kind == 1 ? a.num_q_heads : values0);
       const size_t at = (((size_t)(slot / kPage) * 2 + (kind - 1)) * a.num_kv_heads + head) * kTileWords + (slot % kPage) * kHeadDim;
       if constexpr (F8) {
         uint8_t* dst = static_cast<uint8_t*>(a.pool) + at;
@@ -154,9 +175,14 @@ hipError_t launch_rope(const RopeArgs& a, int dtype, hipStream_t st) {
   if (a.n == 0) return hipSuccess;
   RopeArgs b = a;
   const int rows = a.num_q_heads + 2 * a.num_kv_heads;
-  b.rows_per_wave = a.n >= 2048 ? rows : 8;
-  const int64_t items = (int64_t)a.n * ((rows + b.rows_per_wave - 1) / b.rows_per_wave);
-  const dim3 grid((unsigned)((items + kWaves - 1) / kWaves)), block(64 * kWaves);
+  // A wave works the angles out once for its rows, 8 at a time: as many rows as leave 2048
+  // waves (8 a CU).  Measured with 48 rows a token, us at 8 / 16 / 24 / 48 rows a wave:
+  // 64 tokens 4.2 / 4.6 / 5.0 / 6.5, 512 tokens 6.3 / 5.6 / 6.0 / 7.2, 1024 tokens
+  // 8.5 / 7.2 / 7.0 / 7.8, 8192 tokens 47.8 / 35.5 / 33.8 / 34.6.
+  const int64_t share = ((int64_t)a.n * rows + 2047) / 2048;
+  b.rows_per_wave = (int)std::min<int64_t>((share + 7) / 8 * 8, rows);
+  const int64_t waves = (int64_t)a.n * ((rows + b.rows_per_wave - 1) / b.rows_per_wave);   // (at most 2048 + a.n)
+  const dim3 grid((unsigned)((waves + kWaves - 1) / kWaves)), block(64 * kWaves);
   switch (dtype) {
     case 0: hipLaunchKernelGGL((rope_kernel<Bf16, false>), grid, block, 0, st, b); break;
     case 1: hipLaunchKernelGGL((rope_kernel<Fp16, false>), grid, block, 0, st, b); break;

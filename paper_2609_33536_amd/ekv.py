@@ -434,7 +434,7 @@ def _typed(t, dtype, shape, name):
     size would be read or written past its end."""
     if t is None:
         return None
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+    if t.dtype is not dtype or t.shape != shape:
         raise EkvError(ERR_INVALID, f"{name} must be {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
     return _ptr(t)
 
@@ -493,14 +493,15 @@ def make_rope(turns, rotary_dim, layout="half", magnitude=1.0):
 
 def _rows(t, shape, dtype, name):
     """(pointer, row stride) of a tensor [n][heads][128] whose heads are packed."""
-    if t.dtype != dtype or tuple(t.shape) != shape:
+    if t.dtype is not dtype or t.shape != shape:
         raise EkvError(ERR_INVALID, f"{name} must be {dtype} {shape}, got {t.dtype} {tuple(t.shape)}")
     if not t.is_cuda:
         raise EkvError(ERR_INVALID, "device argument must be a GPU tensor")
-    if t.stride(2) != 1 or t.stride(1) != HEAD_DIM:
+    row, head, value = t.stride()
+    if value != 1 or head != HEAD_DIM:
         raise EkvError(ERR_INVALID, f"the heads of a row of {name} must be packed")
     # (a single row's stride says nothing)
-    return t.data_ptr(), t.stride(0) if shape[0] > 1 else max(t.stride(0), shape[1] * HEAD_DIM)
+    return t.data_ptr(), row if shape[0] > 1 else max(row, shape[1] * HEAD_DIM)
 
 
 def rope_append(pool, rope, positions, slots, q, k, v, q_out, stream=None):

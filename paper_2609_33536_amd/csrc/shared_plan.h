@@ -63,9 +63,15 @@ __host__ __device__ inline SharedPlan divide_work(const SharedWork& n, int grid,
   if (n.team_units > 0 && t == 0) t = 1;
   if (n.few_work > 0 && f == 0) f = 1;
   if (n.own_work > 0 && o == 0) o = 1;
+  // Two tiles on one compute unit run slower than a tile beside streams: a few tiles more
+  // than compute units are not worth it (three 8-bit prefixes of 16384 tokens and 55
+  // sequences of up to 2048: 91.9 us, with the 273 tile workers of the weights alone 97.8).
+  constexpr int cus = kMaxSharedGrid / 2;
+  const bool whole = t > cus && 4 * t < 5 * cus && f + o > 0;
+  if (whole) t = cus;
   // (what rounding left over or took too much)
   const int rest = grid - t - f - o;
-  if (t >= f && t >= o) t += rest;
+  if (t >= f && t >= o && !whole) t += rest;
   else if (f >= o) f += rest;
   else o += rest;
   SharedPlan p{t, f, o, 1, 0, 1, 1};

@@ -52,11 +52,13 @@ struct SharedPlan {
 // Divides `grid` workgroups (at least 4) over the kinds by their units and
 // segments, weighted by what these cost a workgroup: a tile's unit is matrix work
 // of 4 waves, the others' are bytes from HBM (half as many for 8-bit pools); a
-// segment costs its start (table, queries, first loads) and its partials, 5 units of
-// a tile and one of a wave's stream.
+// segment costs its start (table, queries, first loads) and its partials: one unit of
+// a wave's stream, and of a tile 5, or 10 where first loads queue behind streams that
+// use all of HBM's rate (16-bit pools: 64 sequences of up to 2048 behind 64 tokens
+// 95.9 us at 5, 84.5 at 10; 8-bit, 55 of up to 2048 behind 256 tokens 41.0 and 48.4).
 __host__ __device__ inline SharedPlan divide_work(const SharedWork& n, int grid, int min_units, bool bytes8) {
   const float stream = bytes8 ? 1.75f : 2.5f;
-  const float team = 4.f * n.team_units + 20.f * n.team_segments;
+  const float team = 4.f * n.team_units + (bytes8 ? 20.f : 40.f) * n.team_segments;
   const float few = stream * n.few_work, own = stream * n.own_work;
   const float share = grid / fmaxf(1.f, team + few + own);
   int t = (int)(share * team), f = (int)(share * few), o = (int)(share * own);

@@ -436,7 +436,9 @@ def _typed(t, dtype, shape, name):
         return None
     if t.dtype is not dtype or t.shape != shape:
         raise EkvError(ERR_INVALID, f"{name} must be {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
-    return _ptr(t)
+    if t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
+    return _ptr(t)   # (raises)
 
 
 def make_free_list(ids, cursor, num_blocks, cursor_out=None):

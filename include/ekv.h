@@ -725,7 +725,9 @@ ekv_status ekv_rope_append(const ekv_pool* pool, const ekv_rope* rope, int32_t n
  * ws, q, out and the pool are 16-byte aligned.
  * Transitions of a prefix's pairs are made on its row like any sequence's
  * (ekv_demote on the prefixes' table), while no attention call reads it.
- * Errors: as ekv_attn_decode.
+ * Errors: as ekv_attn_decode; EKV_ERR_UNSUPPORTED also for more than 64
+ * sequences for each workgroup that the device holds (two a compute unit, at
+ * most 512: 32768 sequences on all of an MI355X).
  */
 size_t ekv_decode_shared_workspace_bytes(const ekv_pool* pool, const ekv_batch* prefixes, const ekv_batch* batch);
 ekv_status ekv_attn_decode_shared(const ekv_pool* pool, const ekv_batch* prefixes, const int32_t* group_start,

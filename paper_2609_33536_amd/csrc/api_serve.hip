@@ -41,6 +41,8 @@ ekv_status plan_shared(const ekv_pool* p, const ekv_batch* prefixes, const ekv_b
   l->min_units = (int)std::max<int64_t>(1, std::min<int64_t>(4, units_p / 16));   // (of the prefixes: pieces to merge)
   const int64_t wanted = (work_t + hkv * groups * (units_p + 1) / 4 + work_s / 4) / l->min_units + 4;
   l->grid = (int)std::min<int64_t>(kMaxSharedGrid, wanted);
+  if (rows > 64 * l->grid)   // (each workgroup describes 64 sequences to the merge)
+    return fail(EKV_ERR_UNSUPPORTED, "at most %d sequences in one shared-prefix decode call", 64 * kMaxSharedGrid);
   // The merge: a workgroup takes 8 pieces a memory round trip.  Where a column may have more (at
   // most its units, or what is left of the workers for each segment), up to 8 waves divide them, as
   // long as that leaves the launch at most twice the device's workgroups.
@@ -261,8 +263,8 @@ ekv_status ekv_attn_decode_shared(const ekv_pool* pool, const ekv_batch* prefixe
     a.log2_group = __builtin_ctz((unsigned)group);
     a.out_fp32 = out_dtype == EKV_DTYPE_FP32;
     a.grid = std::max(4, std::min(l.grid, resident));
-    if (batch->batch > 64 * a.grid)   // (each workgroup describes 64 sequences to the merge)
-      return fail(EKV_ERR_UNSUPPORTED, "ekv_attn_decode_shared: at most %d sequences", 64 * a.grid);
+    if (batch->batch > 64 * a.grid)
+      return fail(EKV_ERR_UNSUPPORTED, "at most %d sequences in one shared-prefix decode call on this device", 64 * a.grid);
     a.min_units = l.min_units;
     a.merge_ways = l.merge_ways;
     a.scale_log2 = log2e_scale(scale);

@@ -533,6 +533,8 @@ def attn_decode_shared(pool, prefixes, group_start, batch, q, out, scale, ws, st
     """Decode of sequences behind shared prefixes: `prefixes` is a
     :func:`make_batch` of the prefixes' rows, group_start int32
     [prefixes.batch + 1] the first sequence behind each."""
-    _check(lib().ekv_attn_decode_shared(ctypes.byref(pool), ctypes.byref(prefixes), _ptr(group_start),
+    import torch
+    start = _typed(group_start, torch.int32, (prefixes.batch + 1,), "group_start")
+    _check(lib().ekv_attn_decode_shared(ctypes.byref(pool), ctypes.byref(prefixes), start,
                                         ctypes.byref(batch), _ptr(q), _ptr(out), dtype_code(out.dtype), scale, _ptr(ws),
                                         ws.numel() * ws.element_size(), _stream(stream)))

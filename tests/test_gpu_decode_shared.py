@@ -88,6 +88,17 @@ def test_numbers_of_sequences_around_tiles(count):
     _run([300], rng.integers(0, 70, size=count), [0, count], 8, 2, seed=count, base=0.3)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "e5m2"])
+@pytest.mark.parametrize("counts", [[40], [41], [33, 40, 8], [72, 9, 34, 1]])
+def test_columns_left_over_by_tiles(counts, dtype):
+    """G = 4: up to 8 sequences behind full tiles of 32 are streamed (40: one tile and 8
+    sequences; 41: two tiles), for one prefix and several."""
+    rng = np.random.default_rng(sum(counts))
+    start = np.concatenate([[1], 1 + np.cumsum(counts)])
+    own = rng.integers(0, 70, size=int(start[-1]) + 2)
+    _run(rng.integers(200, 900, size=len(counts)), own, start.tolist(), 8, 2, seed=len(own), base=0.3, dtype=dtype)
+
+
 @pytest.mark.parametrize("structured", [True, False])
 @pytest.mark.parametrize("dtype", ["bf16", "e5m2"])
 def test_oldest_half_base_structured_and_general(structured, dtype):

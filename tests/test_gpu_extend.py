@@ -12,21 +12,21 @@ pytestmark = pytest.mark.gpu
 CANARY = -77
 
 
-def _guarded(torch, a, dtype=None):
-    """A device copy of `a` between canary words; returns (view, check)."""
+def _guarded(torch, a, shift=0):
+    """A device copy of `a` between canary words, `shift` words off its 16-byte boundary; returns (view, check)."""
     a = np.ascontiguousarray(a)
-    pad = np.full(16, CANARY & 0x7F, dtype=a.dtype)
+    pad = np.full(16 + shift, CANARY & 0x7F, dtype=a.dtype)
     whole = torch.from_numpy(np.concatenate([pad, a.reshape(-1), pad])).cuda()
-    view = whole[16:16 + a.size].view(a.shape)
+    view = whole[len(pad):len(pad) + a.size].view(a.shape)
 
     def check():
         h = whole.cpu().numpy()
-        assert (h[:16] == pad).all() and (h[len(h) - 16:] == pad).all(), "written outside an array"
+        assert (h[:len(pad)] == pad).all() and (h[len(h) - len(pad):] == pad).all(), "written outside an array"
     return view, check
 
 
 def _run(seq_lens, new_lens, width, *, free=None, spare=5, max_tokens=None, start=None, in_place=False, seed=0,
-         tags=None, head=None, no_new=False, bad_ids=False):
+         tags=None, head=None, no_new=False, bad_ids=False, shift=0):
     torch = require_gpu()
     rng = np.random.default_rng(seed)
     lens, new = np.asarray(seq_lens, dtype=np.int32), np.asarray(new_lens, dtype=np.int32)
@@ -51,8 +51,8 @@ def _run(seq_lens, new_lens, width, *, free=None, spare=5, max_tokens=None, star
 
     checks = []
 
-    def dev(a):
-        v, c = _guarded(torch, a)
+    def dev(a, shift=0):
+        v, c = _guarded(torch, a, shift)
         checks.append(c)
         return v
 
@@ -60,7 +60,7 @@ def _run(seq_lens, new_lens, width, *, free=None, spare=5, max_tokens=None, star
     d_bt, d_tags = dev(table), dev(tags)
     d_cur_out = d_cur if in_place else dev(np.full(2, 9, dtype=np.int32))
     d_out = d_lens if in_place else dev(np.full(b, 9, dtype=np.int32))
-    d_cu, d_slots, d_pos = (dev(np.full(n, 9, dtype=np.int32)) for n in (b + 1, rows, rows))
+    d_cu, d_slots, d_pos = (dev(np.full(n, 9, dtype=np.int32), k) for n, k in ((b + 1, 0), (rows, shift), (rows, shift)))
     d_status = dev(np.full(4, 9, dtype=np.int32))
     d_start = None if start is None else dev(np.asarray(start, dtype=np.int32))
     print(f"extend: B={b} rows={rows} need={need} free={count} in_place={in_place}", flush=True)
@@ -111,6 +111,34 @@ def test_ragged_prompts(seed, in_place):
 
 def test_one_very_long_prompt():
     assert _run([3, 0, 7], [1, 500001, 0], 31260, in_place=True)["status"][0] == 0
+
+
+@pytest.mark.parametrize("shift", [0, 1])
+@pytest.mark.parametrize("extra", [0, 1, 2, 3])
+def test_more_tokens_than_threads(extra, shift):
+    """Beyond 768 x 256 tokens a thread writes four neighbours: sequences of none, one
+    and a few tokens between long ones, a last group that is not whole, rows behind the
+    last token, and arrays that 16-byte stores would miss."""
+    rng = np.random.default_rng(extra)
+    new = np.concatenate([rng.integers(0, 4, size=500), [70001, 0, 0, 1, 130000], rng.integers(0, 40, size=60)])
+    new[-1] += (extra - int(new.sum())) % 4
+    lens = rng.integers(0, 90, size=len(new))
+    want = _run(lens, new, 8200, seed=extra, shift=shift, start=rng.integers(0, 1000, size=len(new)))
+    assert want["status"][0] == 0 and want["status"][1] > 768 * 256 and want["status"][1] % 4 == extra
+
+
+@pytest.mark.parametrize("b", [256, 511, 769, 1024, 1025, 2049])
+def test_numbers_of_sequences_around_a_wave_s_chunks(b):
+    """A wave scans a quarter of the sequences, four chunks of 64 at a time."""
+    rng = np.random.default_rng(b)
+    assert _run(rng.integers(0, 200, size=b), rng.integers(0, 30, size=b), 20, seed=b)["status"][0] == 0
+
+
+def test_a_refusal_among_many_sequences_takes_nothing():
+    for at in (0, 63, 64, 600, 1026):
+        new = np.full(1027, 2)
+        new[at] = -1
+        assert _run(np.full(1027, 7), new, 4, in_place=at % 2 == 0)["status"][0] == ekv.EXTEND_ROW
 
 
 def test_exactly_all_free_blocks_and_rows():

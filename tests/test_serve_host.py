@@ -134,7 +134,8 @@ SHARED = dict(q=AT, out=AT, out_dtype=ekv.DTYPE_FP32, scale=0.1, ws=AT, ws_bytes
     ({}, dict(mode=ekv.MODE_GENERAL), {}, AT, INVALID, "tag"), ({}, {}, dict(mode=ekv.MODE_GENERAL), AT, INVALID, "tag"),
     ({}, {}, dict(num_q_heads=24), AT, UNSUPPORTED, "group"), ({}, {}, dict(num_q_heads=20), AT, INVALID, "multiple"),
     ({}, dict(max_seq_len=129), {}, AT, INVALID, "max_seq_len"), ({}, dict(max_blocks=1 << 26), {}, AT, UNSUPPORTED, "max_blocks"),
-    ({}, dict(max_blocks=1 << 25), dict(batch=1 << 12), AT, UNSUPPORTED, "too large")])
+    ({}, dict(max_blocks=1 << 25), dict(batch=1 << 12), AT, UNSUPPORTED, "too large"),
+    ({}, {}, dict(batch=32769, max_blocks=2), AT, UNSUPPORTED, "at most 32768 sequences")])
 def test_decode_shared_refusals(lib, kw, prefix, own, start, want, word):
     p, b = _batch(**{"batch": 2, **prefix}), _batch(**own)
     _refused(lib, lib.ekv_attn_decode_shared(ctypes.byref(_pool()), ctypes.byref(p), start, ctypes.byref(b),
@@ -167,7 +168,9 @@ def test_bindings_refuse_wrong_tensors():
                 lambda: ekv.make_rope(torch.zeros(32, dtype=torch.int64), 128),
                 lambda: ekv.extend(ekv.FreeList(), i32(2), i32(3), i32(2, 4), None, i32(2), i32(3), i32(8), i32(8), i32(4)),
                 lambda: ekv.rope_append(_pool(num_kv_heads=2), ekv.Rope(), i32(3), i32(3), torch.zeros((3, 8, 128)),
-                                        torch.zeros((3, 2, 128)), torch.zeros((3, 2, 128)), torch.zeros((3, 8, 128)))):
+                                        torch.zeros((3, 2, 128)), torch.zeros((3, 2, 128)), torch.zeros((3, 8, 128))),
+                lambda: ekv.attn_decode_shared(_pool(), _batch(batch=2), i32(2), _batch(), None, None, 0.1, None),
+                lambda: ekv.attn_decode_shared(_pool(), _batch(batch=2), i32(3).long(), _batch(), None, None, 0.1, None)):
         with pytest.raises(ekv.EkvError) as e:
             bad()
         assert e.value.status == INVALID

@@ -191,17 +191,23 @@ struct Stager {
       dma16(src2 + v_off, off, v_slot + at + kGroup);
     }
   }
-  // As widen, for one plane's slot.
-  __device__ __forceinline__ void widen_plane(char* slot, bool base, int q, int lane) const {
-    if (!F8 && !base) return;
-    char* at = slot + quarter_offset(q);
-    u32x4 raw;
+  // As widen, for one plane's slot, in two steps: what landed, and its words in place
+  // (by one wave, which reads all of its quarter before it writes).
+  __device__ __forceinline__ u32x4 landed_plane(const char* slot, bool base, int q, int lane) const {
+    const char* at = slot + quarter_offset(q);
+    if (!F8 && !base) return u32x4{0u, 0u, 0u, 0u};
     if (F8 && base) {
       const u32x2 x = *reinterpret_cast<const u32x2*>(at + raw_n);
-      const u32x2 lo = widen_nibbles(x.x), hi = widen_nibbles(x.y);
+      return u32x4{x.x, x.y, 0u, 0u};
+    }
+    return *reinterpret_cast<const u32x4*>(at + 16 * lane);
+  }
+  __device__ __forceinline__ void widen_plane(char* slot, bool base, int q, u32x4 raw) const {
+    if (!F8 && !base) return;
+    char* at = slot + quarter_offset(q);
+    if (F8 && base) {
+      const u32x2 lo = widen_nibbles(raw.x), hi = widen_nibbles(raw.y);
       raw = u32x4{lo.x, lo.y, hi.x, hi.y};
-    } else {
-      raw = *reinterpret_cast<const u32x4*>(at + 16 * lane);
     }
     *reinterpret_cast<u32x4*>(at + dst) = expand_base8(raw.xy);
     *reinterpret_cast<u32x4*>(at + dst + 16) = expand_base8(raw.zw);

@@ -331,11 +331,17 @@ struct Worker {
       ++issued;
     };
     auto is_base = [&](int u) { return ELASTIC && ((modes >> (issued - 1 - u)) & 1u) != 0u; };
-    auto stage_k = [&](int u) { stager.widen_plane(ring + k_slot(u), is_base(u), wave, lane); };
-    auto stage_v = [&](int u) {
+    // what landed of K of unit u and V of unit u - 1 (this wave's quarters), and its words in place
+    u32x4 raw_k, raw_v;
+    auto take = [&](int u) {
+      raw_k = stager.landed_plane(ring + k_slot(u), is_base(u), wave, lane);
+      raw_v = stager.landed_plane(ring + kVRing + v_stage, is_base(u - 1), wave, lane);
+    };
+    auto stage = [&](int u) {
       char* at = ring + kVRing + next_v(v_stage);
-      stager.widen_plane(at, is_base(u), wave, lane);
-      stager.clear_tail(at, wave, 2 * kPage * (x.u0 + u), x.len);
+      stager.widen_plane(ring + k_slot(u), is_base(u), wave, raw_k);
+      stager.widen_plane(at, is_base(u - 1), wave, raw_v);
+      stager.clear_tail(at, wave, 2 * kPage * (x.u0 + u - 1), x.len);
     };
     // everything but the last 5 planes issued (V of unit i + 2, K and V of i + 3 and i + 4) has landed
     auto landed = [&]() { wait_loads<5 * Stager<F8>::kLoads / 2>(); };
@@ -356,9 +362,10 @@ struct Worker {
 #pragma unroll 1
     for (int u = 0; u < 4; ++u) issue();
     landed();
-    stage_k(0);
-    stage_k(1);
-    stage_v(0);
+    raw_k = stager.landed_plane(ring + k_slot(0), is_base(0), wave, lane);
+    stager.widen_plane(ring + k_slot(0), is_base(0), wave, raw_k);
+    take(1);
+    stage(1);
     barrier();
     read_k(k_at, k);
     f32x16 sc = col.scores(k);
@@ -375,6 +382,8 @@ struct Worker {
         products();
         read_v(v_at + v_now, v);
         const f32x16 next = col.scores(k);
+        landed();
+        take(i + 2);
         u32x4 nhi[2], nlo[2];
         float sum = col.probabilities(sc, c, finite_or_zero(col.m), nhi, nlo);
         // (kept in this block, beside the products: not sunk below the rescale's branch)
@@ -387,10 +396,11 @@ struct Worker {
         sc = next;
         if (moved) col.rescale(shift == shift ? fast_exp2(shift) : 1.0f);   // (unit i - 1's products, under the old reference, are in)
         col.l += sum;
+      } else {
+        landed();
+        take(i + 2);
       }
-      landed();
-      stage_k(i + 2);
-      stage_v(i + 1);
+      stage(i + 2);
     }
     wait_loads<0>();   // no load may land in a slot of the next piece, or after the workgroup has ended
     products();

@@ -443,8 +443,19 @@ struct Worker {
     while (true) {
       const int key0 = 2 * kPage * (x.u0 + i);
       wait_loads<0>();
+      if (F8 || base) {   // (all is read before any of it is widened: one LDS round trip)
+        u32x4 raw[4][2];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) stager.widen(slot, base, q, key0, x.len, lane);
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int pl = 0; pl < 2; ++pl) raw[q][pl] = stager.landed_plane(slot + pl * kPlanePf, base, q, lane);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int pl = 0; pl < 2; ++pl) stager.widen_plane(slot + pl * kPlanePf, base, q, raw[q][pl]);
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) stager.clear_tail(slot + kPlanePf, q, key0, x.len);
       u32x4 k[8], v[2][4], hi[2], lo[2];
       read_k(slot + k_at, k);
       read_v(slot + v_at, v);

@@ -10,7 +10,10 @@
 //
 // 8 lanes hold a head's 128 elements, lane c the pairs 8c .. 8c + 7 (half layout:
 // elements 8c.. and rotary_dim / 2 + 8c..; pair layout: 16c .. 16c + 15), so that a
-// lane's cosines and sines serve every head that its wave turns.
+// lane's cosines and sines serve every head that its wave turns.  The kernel is bound
+// by HBM: q in and out, k and v in, their cache rows out.  16384 tokens of 64 + 2 x 8 heads
+// into an 8-bit pool take 127 us (638 MB, 5.0 TB/s; a plain copy reaches 5.2), 64 tokens of
+// 32 + 2 x 8 heads 4.2 us (a launch).
 #include <algorithm>
 
 #include "common.h"
@@ -75,7 +78,8 @@ __device__ __forceinline__ void floats8(u32x4 w, float (&x)[8]) {
   }
 }
 
-template <typename T, bool F8>
+// ONCE: inputs are read past the caches
+template <typename T, bool F8, bool ONCE>
 __global__ __launch_bounds__(64 * kWaves) void rope_kernel(RopeArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 7;
   const int rows = a.num_q_heads + 2 * a.num_kv_heads;   // rows of a token: query heads, key heads, value heads
@@ -95,8 +99,14 @@ __global__ __launch_bounds__(64 * kWaves) void rope_kernel(RopeArgs a) {
     const uint16_t* src = r < a.num_q_heads ? a.q + token * a.q_stride + (size_t)r * kHeadDim
                           : r < values0     ? a.k + token * a.k_stride + (size_t)(r - a.num_q_heads) * kHeadDim
                                             : a.v + token * a.v_stride + (size_t)(r - values0) * kHeadDim;
-    w0 = *reinterpret_cast<const u32x4*>(src + 8 * chunk0);
-    w1 = *reinterpret_cast<const u32x4*>(src + 8 * chunk1);
+    const u32x4 *p0 = reinterpret_cast<const u32x4*>(src + 8 * chunk0), *p1 = reinterpret_cast<const u32x4*>(src + 8 * chunk1);
+    if constexpr (ONCE) {
+      w0 = __builtin_nontemporal_load(p0);
+      w1 = __builtin_nontemporal_load(p1);
+    } else {
+      w0 = *p0;
+      w1 = *p1;
+    }
   };
   // (the first row's values are on their way while the angles are worked out, the next row's while one is turned)
   int r = row0 + (lane >> 3);
@@ -169,6 +179,12 @@ __global__ __launch_bounds__(64 * kWaves) void rope_kernel(RopeArgs a) {
   }
 }
 
+template <typename T, bool F8>
+void launch_typed(const RopeArgs& a, dim3 grid, dim3 block, bool once, hipStream_t st) {
+  if (once) hipLaunchKernelGGL((rope_kernel<T, F8, true>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((rope_kernel<T, F8, false>), grid, block, 0, st, a);
+}
+
 }  // namespace
 
 hipError_t launch_rope(const RopeArgs& a, int dtype, hipStream_t st) {
@@ -182,11 +198,17 @@ hipError_t launch_rope(const RopeArgs& a, int dtype, hipStream_t st) {
   const int64_t share = ((int64_t)a.n * rows + 2047) / 2048;
   b.rows_per_wave = (int)std::min<int64_t>((share + 7) / 8 * 8, rows);
   const int64_t waves = (int64_t)a.n * ((rows + b.rows_per_wave - 1) / b.rows_per_wave);   // (at most 2048 + a.n)
+  // Inputs of 32 MB and more are read past the caches, which the outputs, read next, then
+  // have to themselves: a copy that makes q, k and v, this kernel and a copy of its queries
+  // take 105.5 us for 8192 tokens of 48 rows (111.3 with plain loads), 58.5 (59.9) for
+  // 4096; 1337 tokens (16 MB) alone, their inputs still cached, 11.9 (9.7).  Stores past the
+  // caches make this kernel 5 % faster and what reads its outputs slower by more.
+  const bool once = (int64_t)a.n * rows * kHeadDim * 2 >= (32 << 20);
   const dim3 grid((unsigned)((waves + kWaves - 1) / kWaves)), block(64 * kWaves);
   switch (dtype) {
-    case 0: hipLaunchKernelGGL((rope_kernel<Bf16, false>), grid, block, 0, st, b); break;
-    case 1: hipLaunchKernelGGL((rope_kernel<Fp16, false>), grid, block, 0, st, b); break;
-    case 3: hipLaunchKernelGGL((rope_kernel<Fp16, true>), grid, block, 0, st, b); break;
+    case 0: launch_typed<Bf16, false>(b, grid, block, once, st); break;
+    case 1: launch_typed<Fp16, false>(b, grid, block, once, st); break;
+    case 3: launch_typed<Fp16, true>(b, grid, block, once, st); break;
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();

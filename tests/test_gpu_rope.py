@@ -136,6 +136,13 @@ def test_in_place_and_packed_rows(dtype, packed, n):
     _run(n, 8, 4, dtype=dtype, packed=packed, in_place=True, layout="pairs" if packed else "half", rot=96, seed=21)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "e5m2"])
+@pytest.mark.parametrize("n,packed,in_place", [(2047, False, False), (2048, False, True), (2050, True, True)])
+def test_inputs_around_32_megabytes(dtype, n, packed, in_place):
+    """64 rows of 256 bytes a token: from 2048 tokens on the inputs are read past the caches."""
+    _run(n, 40, 12, dtype=dtype, packed=packed, in_place=in_place, layout="pairs" if packed else "half", seed=n)
+
+
 def test_slots_outside_the_pool_leave_it_as_it_is():
     _run(20, 4, 2, seed=3, skip=[(0, -1), (7, -2**31), (11, 16 * 5), (12, 16 * 5 + 15), (19, 2**31 - 1)], nb=5)
 

@@ -14,7 +14,7 @@
 // cursor may be updated in place: one workgroup does so behind a barrier; of
 // several, all of which read them, none may, and a second launch of one does.
 // Bound by latency: 64 single tokens 4.0 us (an empty launch takes 4.1 back to back),
-// 192 sequences with 25 thousand tokens 4.8, 512 prompts with 260 thousand 7.1.
+// 192 sequences with 24 thousand tokens 4.8, 512 prompts with 538 thousand 7.1.
 #include "common.h"
 #include "extend.h"
 #include "wave_scan.h"
@@ -220,7 +220,7 @@ __global__ __launch_bounds__(kThreads) void extend_kernel(ExtendArgs a) {
 }  // namespace
 
 hipError_t launch_extend(const ExtendArgs& a, hipStream_t st) {
-  // One token a thread up to three workgroups a CU (48 KB of LDS each; 524288 tokens: 7.1 us,
+  // One token a thread up to three workgroups a CU (48 KB of LDS each; 538 thousand tokens: 7.1 us,
   // with 512 and 256 workgroups 8.9 and 10.7).  In place, one workgroup does for 2048
   // tokens: 5.3 us, where 8 take 3.9 and the second launch as much again.
   const bool in_place = a.lens_out == a.lens || a.cursor_out == a.cursor;

@@ -168,6 +168,9 @@ def _host(a, dtype):
     return a, a.ctypes.data_as(ctypes.c_void_p)
 
 
+_current = None   # torch's functions for the current stream and device, once it has initialised the GPU
+
+
 def _stream(stream):
     """The HIP stream handle of a torch stream, or of the current one.  The
     current stream's handle is asked for directly: building the
@@ -175,10 +178,14 @@ def _stream(stream):
     (the handle alone 0.2), which bounds the smallest calls."""
     if stream is not None:
         return stream.cuda_stream
-    import torch
-    if torch.cuda.is_initialized():
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
-    return torch.cuda.current_stream().cuda_stream
+    global _current
+    if _current is None:
+        import torch
+        if not torch.cuda.is_initialized():
+            return torch.cuda.current_stream().cuda_stream
+        _current = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+    raw, device = _current
+    return raw(device())
 
 
 _DTYPE_CODES = {}

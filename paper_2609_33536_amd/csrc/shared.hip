@@ -605,7 +605,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     const bool describes = pass == 1 && wave == 0 && 64 * chunk < a.own.rows;
     Describe d{int4{0, 0, 0, 0}, int4{0, 0, 1, 0}, int4{0, 0, 0, 0}};
     int from = 0, work = 0, slots = 0, other_work = 0, other_slots = 0;
-    const bool one = a.prefix.rows == 1;   // (in scalars, without a scan: a third of the time)
+    const bool one = a.prefix.rows == 1;   // (in scalars, without a scan)
     if (one) {
       const int4 v = *rows0;
       const int start = lane_value(v.x, 0);

@@ -73,6 +73,7 @@ CTRL_EAGER_PROMOTION, CTRL_NO_PROMOTION = 1, 2
 
 # reasons of ekv_extend (bits of its status[0])
 EXTEND_ROW, EXTEND_TOKENS, EXTEND_BLOCKS, EXTEND_BASE = 1, 2, 4, 8
+EXTEND_BATCH = 4096   # most sequences of one call
 ROPE_LAYOUTS = {"half": 0, "pairs": 1}
 ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "parts": 3}
 

@@ -222,8 +222,10 @@ class PagedKV:
         import torch
         with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
             new_lens = np.asarray(new_lens, dtype=np.int32)
+            rows = int(new_lens.sum(dtype=np.int64))
+            if len(new_lens) > ekv.EXTEND_BATCH or rows >= 1 << 30:   # (before the mirror changes)
+                raise ekv.EkvError(ekv.ERR_UNSUPPORTED, f"at most {ekv.EXTEND_BATCH} sequences and 2^30 - 1 new tokens")
             taken = self.mirror.plan_extend(new_lens)
-            rows = int(new_lens.sum())
             # one upload: the new lengths, the blocks taken, and the cursor over them
             up = self._upload(np.concatenate([new_lens, taken, np.array([0, 0, len(taken)], dtype=np.int32)]))
             b = len(new_lens)

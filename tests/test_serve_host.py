@@ -1,6 +1,6 @@
 """The serving-step entry points without a GPU: their refusals, each before
 anything is enqueued, with a message; the rotary table against the oracle;
-workspace sizes; the division of workers over the kinds of work."""
+workspace sizes."""
 
 import ctypes
 
@@ -8,7 +8,7 @@ import numpy as np
 import pytest
 
 from oracle import serve
-from paper_2609_33536_amd import ekv
+from paper_2609_33536_amd import ekv, kvpool
 
 INVALID, UNSUPPORTED = ekv.ERR_INVALID, ekv.ERR_UNSUPPORTED
 AT = 0x10000   # a non-NULL, 16-byte aligned address that no refused call reads
@@ -185,3 +185,13 @@ def test_binding_refuses_rows_beyond_32_bits():
     with pytest.raises(ekv.EkvError) as e:
         ekv.extend(ekv.FreeList(), i32(2), i32(2), i32(2, 4), None, i32(2), i32(3), Long(), None, i32(4))
     assert e.value.status == UNSUPPORTED
+
+
+@pytest.mark.parametrize("b,new", [(4097, 1), (1100, 1 << 20)])
+def test_paged_kv_refuses_what_one_call_cannot_extend_before_its_mirror_changes(b, new):
+    kv = object.__new__(kvpool.PagedKV)   # (no device: the refusal comes first)
+    kv.mirror = kvpool.HostMirror(np.zeros((b, 1), dtype=np.int32), np.zeros(b, dtype=np.int32), 8, [3, 4, 5])
+    with pytest.raises(ekv.EkvError) as e:
+        kv.extend(np.full(b, new))
+    assert e.value.status == UNSUPPORTED
+    assert list(kv.mirror.free) == [3, 4, 5] and not kv.mirror.seq_lens.any()

@@ -16,6 +16,7 @@ through :mod:`ekv`.
 """
 
 import contextlib
+import itertools
 from collections import deque
 
 import numpy as np
@@ -100,11 +101,10 @@ class HostMirror:
         self.publish_refine(pairs, new)
         return new
 
-    def plan_extend(self, new_lens):
-        """Give every sequence cache room for new_lens[s] more tokens: blocks
-        from the head of the free pool, sequence by sequence, as TARGET.
-        Returns the blocks taken, in order; nothing changes if they do not
-        fit."""
+    def _extension(self, new_lens):
+        """The blocks (from the head of the free pool, sequence by sequence),
+        their table places and the lengths of an extension; raises if it does
+        not fit and changes nothing."""
         new_lens = np.asarray(new_lens, dtype=np.int32)
         total = self.seq_lens.astype(np.int64) + new_lens
         if new_lens.shape != self.seq_lens.shape or (new_lens < 0).any() or (total > self.bt.shape[1] * self.page).any():
@@ -114,13 +114,26 @@ class HostMirror:
         n = int(need.sum())
         if n > len(self.free):
             raise ekv.EkvError(ekv.ERR_INVALID, f"{n} blocks needed, {len(self.free)} free")
-        taken = np.array([self.free.popleft() for _ in range(n)], dtype=np.int32)
+        taken = np.array(list(itertools.islice(self.free, n)), dtype=np.int32)
         s = np.repeat(np.arange(len(need)), need)
         i = old[s] + np.arange(n) - np.repeat(np.cumsum(need) - need, need)
-        self.bt[s, i] = taken
-        self.tags[s, i] = 0
-        self.seq_lens = total.astype(np.int32)
-        return taken
+        return taken, (s, i), total.astype(np.int32)
+
+    def _publish_extension(self, taken, place, total):
+        for _ in taken:
+            self.free.popleft()
+        self.bt[place] = taken
+        self.tags[place] = 0
+        self.seq_lens = total
+
+    def plan_extend(self, new_lens):
+        """Give every sequence cache room for new_lens[s] more tokens: blocks
+        from the head of the free pool, sequence by sequence, as TARGET.
+        Returns the blocks taken, in order; nothing changes if they do not
+        fit."""
+        extension = self._extension(new_lens)
+        self._publish_extension(*extension)
+        return extension[0]
 
     def lower(self):
         return ekv.lower(self.tags, self.seq_lens, self.page)
@@ -216,16 +229,19 @@ class PagedKV:
 
     def extend(self, new_lens, start=None, stream=None):
         """Cache room for new_lens[s] more tokens of every sequence: table, tags
-        and lengths grow in the mirror and, by one launch, on the device.
-        Returns (cu_q, slots, positions) on the device, a row per new token;
-        positions count from start[s] (device int32, default 0)."""
+        and lengths grow on the device and, once that is enqueued, in the mirror
+        (a call that raises changes neither).  Returns (cu_q, slots, positions)
+        on the device, a row per new token; positions count from start[s]
+        (device int32, default 0)."""
         import torch
         with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
             new_lens = np.asarray(new_lens, dtype=np.int32)
             rows = int(new_lens.sum(dtype=np.int64))
             if len(new_lens) > ekv.EXTEND_BATCH or rows >= 1 << 30:   # (before the mirror changes)
                 raise ekv.EkvError(ekv.ERR_UNSUPPORTED, f"at most {ekv.EXTEND_BATCH} sequences and 2^30 - 1 new tokens")
-            taken = self.mirror.plan_extend(new_lens)
+            ekv._typed(start, torch.int32, (len(new_lens),), "start")   # (before anything is enqueued)
+            extension = self.mirror._extension(new_lens)
+            taken = extension[0]
             # one upload: the new lengths, the blocks taken, and the cursor over them
             up = self._upload(np.concatenate([new_lens, taken, np.array([0, 0, len(taken)], dtype=np.int32)]))
             b = len(new_lens)
@@ -234,6 +250,7 @@ class PagedKV:
             cu_q, slots, positions = out[:b + 1], out[b + 1:b + 1 + rows], out[b + 1 + rows:b + 1 + 2 * rows]
             ekv.extend(free, self.seq_lens, up[:b], self.bt, self.tags, self.seq_lens, cu_q, slots, positions, out[-4:],
                        start, stream)
+            self.mirror._publish_extension(*extension)
         return cu_q, slots, positions
 
 

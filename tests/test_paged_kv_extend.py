@@ -1,0 +1,76 @@
+"""PagedKV.extend without a GPU: a call that raises at any step leaves the mirror
+as it was, so that mirror and device never part."""
+
+import numpy as np
+import pytest
+
+from paper_2609_33536_amd import ekv, kvpool
+
+torch = pytest.importorskip("torch")
+
+
+class _Kv(kvpool.PagedKV):
+    """The state of a PagedKV over CPU tensors; uploads are plain copies."""
+
+    def __init__(self, seq_lens, width=4, free=(7, 8, 9), tags=None):
+        table = np.arange(len(seq_lens) * width, dtype=np.int32).reshape(-1, width) + 100
+        self.mirror = kvpool.HostMirror(table, seq_lens, 64, free, tags)
+        self.bt, self.tags, self.seq_lens = (torch.from_numpy(a.copy()) for a in (self.mirror.bt, self.mirror.tags, self.mirror.seq_lens))
+        self.device = "cpu"
+
+    def _upload(self, arr):
+        return torch.from_numpy(np.ascontiguousarray(arr))
+
+
+def _state(m):
+    return m.bt.tolist(), m.tags.tolist(), m.seq_lens.tolist(), list(m.free)
+
+
+@pytest.fixture
+def kv():
+    return _Kv([0, 20])
+
+
+@pytest.mark.parametrize("start", [torch.tensor([0, 5]), torch.tensor([0, 5, 6], dtype=torch.int32),
+                                   torch.tensor([0.0, 5.0]), torch.tensor([[0, 5]], dtype=torch.int32),
+                                   torch.tensor([0, 5], dtype=torch.int32)],   # (the last one: host memory)
+                         ids=["int64", "length", "float", "shape", "host"])
+def test_a_start_that_is_refused_leaves_the_mirror(kv, start):
+    before = _state(kv.mirror)
+    with pytest.raises(ekv.EkvError, match="start|GPU tensor") as e:
+        kv.extend([3, 20], start)
+    assert e.value.status == ekv.ERR_INVALID
+    assert _state(kv.mirror) == before
+
+
+@pytest.mark.parametrize("step", ["upload", "memory", "launch"])
+def test_a_step_that_fails_leaves_the_mirror(kv, step, monkeypatch):
+    def fail(*a, **k):
+        raise RuntimeError("out of memory")
+    before = _state(kv.mirror)
+    if step == "upload":
+        monkeypatch.setattr(kv, "_upload", fail)
+    elif step == "memory":
+        monkeypatch.setattr(torch, "empty", fail)
+    else:
+        monkeypatch.setattr(ekv, "make_free_list", lambda *a: None)
+        monkeypatch.setattr(ekv, "extend", fail)
+    with pytest.raises(RuntimeError):
+        kv.extend([3, 20])
+    assert _state(kv.mirror) == before
+
+
+def test_the_mirror_follows_the_launch(kv, monkeypatch):
+    """The call's arguments are those of the extension that the mirror then shows."""
+    seen = {}
+    monkeypatch.setattr(ekv, "make_free_list", lambda ids, cursor, blocks: seen.update(ids=ids.tolist(), cursor=cursor.tolist()))
+
+    def launch(free, lens, new, *rest):
+        seen.update(lens=lens.tolist(), new=new.tolist(), mirror=_state(kv.mirror))
+    monkeypatch.setattr(ekv, "extend", launch)
+    before = _state(kv.mirror)
+    kv.extend([3, 20])
+    assert seen["mirror"] == before and seen["lens"] == [0, 20] and seen["new"] == [3, 20]
+    assert seen["ids"][:2] == [7, 8] and seen["cursor"] == [0, 2]
+    assert kv.mirror.seq_lens.tolist() == [3, 40] and list(kv.mirror.free) == [9]
+    assert kv.mirror.bt[0, 0] == 7 and kv.mirror.bt[1, 2] == 8

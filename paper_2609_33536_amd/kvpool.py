@@ -114,6 +114,9 @@ class HostMirror:
         n = int(need.sum())
         if n > len(self.free):
             raise ekv.EkvError(ekv.ERR_INVALID, f"{n} blocks needed, {len(self.free)} free")
+        grows = np.flatnonzero((new_lens > 0) & (self.seq_lens % self.page > 0))
+        if self.tags[grows, self.seq_lens[grows] // self.page].any():
+            raise ekv.EkvError(ekv.ERR_INVALID, "new tokens would go into a partly filled BASE block")
         taken = np.array(list(itertools.islice(self.free, n)), dtype=np.int32)
         s = np.repeat(np.arange(len(need)), need)
         i = old[s] + np.arange(n) - np.repeat(np.cumsum(need) - need, need)

@@ -74,3 +74,15 @@ def test_the_mirror_follows_the_launch(kv, monkeypatch):
     assert seen["ids"][:2] == [7, 8] and seen["cursor"] == [0, 2]
     assert kv.mirror.seq_lens.tolist() == [3, 40] and list(kv.mirror.free) == [9]
     assert kv.mirror.bt[0, 0] == 7 and kv.mirror.bt[1, 2] == 8
+
+
+def test_new_tokens_never_go_into_a_base_block():
+    """The device takes nothing where a partly filled block is tagged BASE: neither does the mirror."""
+    tags = np.zeros((3, 4), dtype=np.uint8)
+    tags[:, 1] = 1
+    m = kvpool.HostMirror(np.arange(12).reshape(3, 4), [32, 20, 0], 64, [20, 21, 22], tags)
+    before = _state(m)
+    with pytest.raises(ekv.EkvError, match="BASE") as e:
+        m.plan_extend([0, 1, 1])
+    assert e.value.status == ekv.ERR_INVALID and _state(m) == before
+    assert m.plan_extend([1, 0, 1]).tolist() == [20, 21]   # (full BASE blocks, and rows that do not grow, are no reason)

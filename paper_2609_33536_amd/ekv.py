@@ -140,6 +140,11 @@ def _check(status):
         raise EkvError(status, f"{L.ekv_status_string(status).decode()}: {L.ekv_last_error().decode()}")
 
 
+def debug_mode():
+    """Whether EKV_DEBUG asks for the checks that synchronise."""
+    return os.environ.get("EKV_DEBUG", "0") not in ("", "0")
+
+
 def _ptr(t):
     """Device pointer of a contiguous torch GPU tensor, or None.  A CPU
     tensor is refused here: its address is host memory no kernel may read

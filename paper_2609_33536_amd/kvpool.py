@@ -235,7 +235,10 @@ class PagedKV:
         and lengths grow on the device and, once that is enqueued, in the mirror
         (a call that raises changes neither).  Returns (cu_q, slots, positions)
         on the device, a row per new token; positions count from start[s]
-        (device int32, default 0)."""
+        (device int32, default 0).  The call's status (ekv_extend: its reasons
+        first) stays on the device in ``extend_status``: the device takes nothing
+        if its arrays were changed behind the mirror's back.  With EKV_DEBUG=1
+        the call waits for the status and raises if it did."""
         import torch
         with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
             new_lens = np.asarray(new_lens, dtype=np.int32)
@@ -253,6 +256,11 @@ class PagedKV:
             cu_q, slots, positions = out[:b + 1], out[b + 1:b + 1 + rows], out[b + 1 + rows:b + 1 + 2 * rows]
             ekv.extend(free, self.seq_lens, up[:b], self.bt, self.tags, self.seq_lens, cu_q, slots, positions, out[-4:],
                        start, stream)
+            self.extend_status = out[-4:]
+            if ekv.debug_mode():
+                reasons = int(self.extend_status[0])
+                if reasons:
+                    raise ekv.EkvError(ekv.ERR_INVALID, f"the extension took nothing on the device (reasons {reasons})")
             self.mirror._publish_extension(*extension)
         return cu_q, slots, positions
 

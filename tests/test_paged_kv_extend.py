@@ -86,3 +86,20 @@ def test_new_tokens_never_go_into_a_base_block():
         m.plan_extend([0, 1, 1])
     assert e.value.status == ekv.ERR_INVALID and _state(m) == before
     assert m.plan_extend([1, 0, 1]).tolist() == [20, 21]   # (full BASE blocks, and rows that do not grow, are no reason)
+
+
+def test_what_the_device_refused_is_there_to_read(kv, monkeypatch):
+    """The status of the last extension is kept on the device; with EKV_DEBUG=1 a refusal raises and the mirror
+    stays, as the device did."""
+    def launch(free, lens, new, bt, tags, out, cu, slots, pos, status, *rest):
+        status.copy_(torch.tensor(reply, dtype=torch.int32))
+    monkeypatch.setattr(ekv, "make_free_list", lambda *a: None)
+    monkeypatch.setattr(ekv, "extend", launch)
+    before, reply = _state(kv.mirror), [ekv.EXTEND_ROW, 0, 0, 2]
+    monkeypatch.setenv("EKV_DEBUG", "1")
+    with pytest.raises(ekv.EkvError, match="took nothing"):
+        kv.extend([3, 20])
+    assert _state(kv.mirror) == before
+    reply = [0, 23, 2, 0]
+    kv.extend([3, 20])
+    assert kv.extend_status.tolist() == reply and kv.mirror.seq_lens.tolist() == [3, 40]

@@ -252,8 +252,10 @@ class PagedKV:
             up = self._upload(np.concatenate([new_lens, taken, np.array([0, 0, len(taken)], dtype=np.int32)]))
             b = len(new_lens)
             free = ekv.make_free_list(up[b:b + len(taken) + 1], up[-2:], self.mirror.num_blocks)
-            out = torch.empty(b + 1 + 2 * rows + 4, dtype=torch.int32, device=self.device)
-            cu_q, slots, positions = out[:b + 1], out[b + 1:b + 1 + rows], out[b + 1 + rows:b + 1 + 2 * rows]
+            # (slots and positions begin on 16 bytes, as the wide stores of long prompts need)
+            wide = (rows + 3) // 4 * 4
+            out = torch.empty(2 * wide + b + 1 + 4, dtype=torch.int32, device=self.device)
+            slots, positions, cu_q = out[:rows], out[wide:wide + rows], out[2 * wide:2 * wide + b + 1]
             ekv.extend(free, self.seq_lens, up[:b], self.bt, self.tags, self.seq_lens, cu_q, slots, positions, out[-4:],
                        start, stream)
             self.extend_status = out[-4:]

@@ -103,3 +103,23 @@ def test_what_the_device_refused_is_there_to_read(kv, monkeypatch):
     reply = [0, 23, 2, 0]
     kv.extend([3, 20])
     assert kv.extend_status.tolist() == reply and kv.mirror.seq_lens.tolist() == [3, 40]
+
+
+@pytest.mark.parametrize("b", [1, 2, 3, 4])
+@pytest.mark.parametrize("new", [0, 1, 3, 4, 45])
+def test_slots_and_positions_are_aligned_for_the_wide_stores(b, new, monkeypatch):
+    kv, seen = _Kv([0] * b, free=range(20)), {}
+    monkeypatch.setattr(ekv, "make_free_list", lambda *a: None)
+    monkeypatch.setattr(ekv, "extend", lambda free, lens, n, bt, tags, out, cu, slots, pos, status, *rest: seen.update(
+        slots=slots, pos=pos, cu=cu, status=status))
+    cu, slots, positions = kv.extend([new] * b)
+    assert slots is seen["slots"] and positions is seen["pos"] and cu is seen["cu"]
+    assert slots.numel() == positions.numel() == b * new and cu.numel() == b + 1 and seen["status"].numel() == 4
+    spans = []
+    for t in (slots, positions, cu, seen["status"]):
+        if t.numel():
+            spans.append((t.data_ptr(), t.data_ptr() + 4 * t.numel()))
+    for t in (slots, positions):
+        assert t.numel() == 0 or t.data_ptr() % 16 == 0
+    spans.sort()
+    assert all(a[1] <= c[0] for a, c in zip(spans, spans[1:]))

@@ -545,9 +545,15 @@ def decode_shared_workspace(pool, prefixes, batch, device="cuda"):
 def attn_decode_shared(pool, prefixes, group_start, batch, q, out, scale, ws, stream=None):
     """Decode of sequences behind shared prefixes: `prefixes` is a
     :func:`make_batch` of the prefixes' rows, group_start int32
-    [prefixes.batch + 1] the first sequence behind each."""
+    [prefixes.batch + 1] the first sequence behind each, q and out
+    [batch.batch][Hq][128]."""
     import torch
     start = _typed(group_start, torch.int32, (prefixes.batch + 1,), "group_start")
+    if q is None or out is None:
+        raise EkvError(ERR_INVALID, "q and out are required")
+    shape = (batch.batch, batch.num_q_heads, HEAD_DIM)
+    dtype = torch.bfloat16 if pool.dtype == DTYPE_BF16 else torch.float16
+    qp, op = _typed(q, dtype, shape, "q"), _typed(out, torch.float32 if out.dtype is torch.float32 else dtype, shape, "out")
     _check(lib().ekv_attn_decode_shared(ctypes.byref(pool), ctypes.byref(prefixes), start,
-                                        ctypes.byref(batch), _ptr(q), _ptr(out), dtype_code(out.dtype), scale, _ptr(ws),
+                                        ctypes.byref(batch), qp, op, dtype_code(out.dtype), scale, _ptr(ws),
                                         ws.numel() * ws.element_size(), _stream(stream)))

@@ -513,10 +513,9 @@ def _rows(t, shape, dtype, name):
     if not t.is_cuda:
         raise EkvError(ERR_INVALID, "device argument must be a GPU tensor")
     row, head, value = t.stride()
-    if value != 1 or head != HEAD_DIM:
+    if value != 1 or (head != HEAD_DIM and shape[1] > 1):   # (a single head's stride says nothing, nor a single row's)
         raise EkvError(ERR_INVALID, f"the heads of a row of {name} must be packed")
-    # (a single row's stride says nothing)
-    return t.data_ptr(), row if shape[0] > 1 else max(row, shape[1] * HEAD_DIM)
+    return t.data_ptr(), row if shape[0] > 1 else shape[1] * HEAD_DIM
 
 
 def rope_append(pool, rope, positions, slots, q, k, v, q_out, stream=None):

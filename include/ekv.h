@@ -441,10 +441,14 @@ ekv_status ekv_check_transition(int32_t kind, const int32_t* h_pairs, int32_t n,
  * the entry i of the pairs / new_blocks list.
  * Asynchronous on the stream; nothing else is written.
  *
- * With EKV_DEBUG=1 in the environment, ekv_attn_decode, ekv_attn_prefill
- * and every transition call run these checks first, synchronise the stream,
- * and return EKV_ERR_INVALID (naming the first violation) without
- * enqueuing anything else.  That mode reports into a static 48-byte device
+ * With EKV_DEBUG=1 in the environment, ekv_attn_decode, ekv_attn_prefill,
+ * ekv_attn_decode_shared (for its prefixes and its batch) and every transition
+ * call run these checks first, synchronise the stream, and return
+ * EKV_ERR_INVALID (naming the first violation) without enqueuing anything
+ * else; so do ekv_extend for a free list that names a block twice, or one
+ * that a sequence of the table holds, and ekv_rope_append for a slot given to
+ * two rows (both copy these arrays to the host and check them there).
+ * The checks above report into a static 96-byte device
  * array of the library (one per device; calls in this mode from several
  * host threads on one device race on it) and is meant for debugging only.
  */
@@ -586,7 +590,7 @@ ekv_status ekv_ctrl_promotion(const ekv_ctrl_config* cfg, ekv_ctrl_state* st, in
  * the same state).  Blocks are given out from the head, first in first out;
  * the caller appends returned ones (a demotion's freed list, a finished
  * sequence's blocks) behind the last and raises the count, ordered with the
- * calls on the stream.  A head outside the ring is taken modulo the capacity
+ * calls on the stream.  No block may be in the list twice, or in use.  A head outside the ring is taken modulo the capacity
  * and a count outside [0, capacity] clamped into it.
  */
 typedef struct {

@@ -3,6 +3,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <vector>
 
 #include "common.h"
 #include "ekv.h"
@@ -96,6 +97,61 @@ SharedPart shared_part(const ekv_pool* pool, const ekv_batch* b) {
   return p;
 }
 
+// ---- EKV_DEBUG: what the arrays of a call must not hold twice ------------
+
+// An array of the device, once the stream has reached it.
+ekv_status debug_read(const int32_t* from, size_t n, std::vector<int32_t>* to, hipStream_t stream, const char* call) {
+  to->resize(n);
+  hipError_t e = n ? hipMemcpyAsync(to->data(), from, n * sizeof(int32_t), hipMemcpyDeviceToHost, stream) : hipSuccess;
+  if (e == hipSuccess) e = hipStreamSynchronize(stream);
+  return e == hipSuccess ? EKV_OK : hip_status(e, call);
+}
+
+// Two rows that would write one token's K and V.
+ekv_status debug_check_slots(const ekv_pool* pool, int32_t n, const int32_t* slots, hipStream_t stream, const char* call) {
+  std::vector<int32_t> at;
+  const ekv_status st = debug_read(slots, (size_t)n, &at, stream, call);
+  if (st != EKV_OK) return st;
+  at.erase(std::remove_if(at.begin(), at.end(), [&](int32_t s) { return s < 0 || s / kPage >= pool->num_blocks; }), at.end());
+  std::sort(at.begin(), at.end());
+  const auto twice = std::adjacent_find(at.begin(), at.end());
+  if (twice != at.end()) return fail(EKV_ERR_INVALID, "%s (EKV_DEBUG): token slot %d for two rows", call, *twice);
+  return EKV_OK;
+}
+
+// A free block that is listed twice, or that a sequence still holds.
+ekv_status debug_check_free(const ExtendArgs& a, hipStream_t stream, const char* call) {
+  if ((long long)a.batch * a.max_blocks >= (1LL << 31))
+    return fail(EKV_ERR_UNSUPPORTED, "%s (EKV_DEBUG): batch * max_blocks must be below 2^31", call);
+  std::vector<int32_t> cursor, ids, lens, table;
+  ekv_status st;
+  if ((st = debug_read(a.cursor, 2, &cursor, stream, call)) != EKV_OK ||
+      (st = debug_read(a.ids, (size_t)a.capacity, &ids, stream, call)) != EKV_OK ||
+      (st = debug_read(a.lens, (size_t)a.batch, &lens, stream, call)) != EKV_OK ||
+      (st = debug_read(a.bt, (size_t)a.batch * a.max_blocks, &table, stream, call)) != EKV_OK)
+    return st;
+  const int count = std::min(std::max(cursor[1], 0), a.capacity);
+  int head = cursor[0] % a.capacity;
+  if (head < 0) head += a.capacity;
+  std::vector<int32_t> open;
+  for (int k = 0; k < count; ++k) {
+    const int32_t id = ids[((size_t)head + k) % a.capacity];
+    if (id >= 0 && id < a.num_blocks) open.push_back(id);   // (outside the pool: no slot)
+  }
+  std::sort(open.begin(), open.end());
+  const auto twice = std::adjacent_find(open.begin(), open.end());
+  if (twice != open.end()) return fail(EKV_ERR_INVALID, "%s (EKV_DEBUG): block %d is in the free list twice", call, *twice);
+  for (int s = 0; s < a.batch; ++s) {
+    const int len = (int)std::min<int64_t>(std::max(lens[s], 0), (int64_t)a.max_blocks * kPage);
+    for (int b = 0; b < (len + kPage - 1) / kPage; ++b) {
+      const int32_t id = table[(size_t)s * a.max_blocks + b];
+      if (std::binary_search(open.begin(), open.end(), id))
+        return fail(EKV_ERR_INVALID, "%s (EKV_DEBUG): block %d is free and held by sequence %d", call, id, s);
+    }
+  }
+  return EKV_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -136,6 +192,8 @@ ekv_status ekv_extend(const ekv_free_list* free_list, int32_t batch, int32_t max
     a.batch = batch;
     a.max_blocks = max_blocks;
     a.max_tokens = max_tokens;
+    const ekv_status st = debug_mode() ? debug_check_free(a, stream, "ekv_extend") : EKV_OK;
+    if (st != EKV_OK) return st;
     return hip_status(launch_extend(a, stream), "ekv_extend launch");
   });
 }
@@ -192,6 +250,7 @@ ekv_status ekv_rope_append(const ekv_pool* pool, const ekv_rope* rope, int32_t n
     if ((q_stride | q_out_stride | k_stride | v_stride) % 8 || !aligned16(q) || !aligned16(k) || !aligned16(v) ||
         !aligned16(q_out) || !aligned16(pool->kv))
       return fail(EKV_ERR_INVALID, "rows must be 16-byte aligned");
+    if (debug_mode() && (st = debug_check_slots(pool, n, slots, stream, "ekv_rope_append")) != EKV_OK) return st;
     RopeArgs a{};
     a.positions = positions;
     a.slots = slots;

@@ -22,44 +22,19 @@ bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0;
 // ---- shared-prefix decode -------------------------------------------------
 
 // Scratch of a call: [12 ints a sequence for the merge | (m, l) and o of 32-column slots | of G-column slots],
-// 256-B aligned parts.  Slots: at most one per 32 columns (or part of 32) of a group
-// and KV head, and 4 per workgroup for the segments that workers cut; likewise one
-// per sequence and KV head.
-struct SharedLayout {
-  int grid, min_units, merge_ways;
-  int64_t wide_slots, own_slots;
+// 256-B aligned parts.
+struct SharedLayout : SharedSize {
   size_t ml_wide, o_wide, ml_own, o_own, total;
 };
 
 ekv_status plan_shared(const ekv_pool* p, const ekv_batch* prefixes, const ekv_batch* b, int group, SharedLayout* l) {
-  const int64_t hkv = p->num_kv_heads, rows = b->batch, columns = rows * group;
-  const int64_t groups = std::min<int64_t>(prefixes->batch, rows);
   const int64_t units_p = (max_seq_blocks(prefixes) + 1) / 2, units_s = (max_seq_blocks(b) + 1) / 2;
-  const int64_t tiles = columns / 128 + groups;
-  const int64_t work_t = hkv * tiles * (units_p + 1), work_s = hkv * rows * (units_s + 1);   // (a segment's start counts too)
-  if (work_t >= (1 << 30) || work_s >= (1 << 30) || columns * hkv >= (1 << 30) || prefixes->batch >= (1 << 24))
+  if (!size_shared(prefixes->batch, b->batch, units_p, units_s, p->num_kv_heads, group, l))
     return fail(EKV_ERR_UNSUPPORTED, "batch too large for one shared-prefix decode call");
-  // The fewest units that a worker takes of a prefix, so that short prefixes leave the merge fewer
-  // pieces: with 1 instead, 64 sequences behind 2048 tokens take 27.4 us (25.3), 8 behind 8192 23.7
-  // (21.5), longer and shorter ones the same.
-  l->min_units = (int)std::max<int64_t>(1, std::min<int64_t>(4, units_p / 16));
-  const int64_t wanted = (work_t + hkv * groups * (units_p + 1) / 4 + work_s / 4) / l->min_units + 4;
-  l->grid = (int)std::min<int64_t>(kMaxSharedGrid, wanted);
-  if (rows > 64 * l->grid)   // (each workgroup describes 64 sequences to the merge)
+  if (b->batch > 64 * l->grid)   // (each workgroup describes 64 sequences to the merge)
     return fail(EKV_ERR_UNSUPPORTED, "at most %d sequences in one shared-prefix decode call", 64 * kMaxSharedGrid);
-  // The merge: a workgroup takes 8 pieces a memory round trip.  Where a column may have more (at
-  // most its units, or what is left of the workers for each segment), up to 8 waves divide them, as
-  // long as the launch has at most one workgroup a compute unit.  With one wave always, 8 sequences
-  // behind 32768 tokens take 68.5 us (39.1), 4 behind 512 14.2 (12.6); with up to two workgroups a
-  // compute unit 16 prompts with samples take 66.8 (64.4).
-  const int64_t pieces = std::min(units_p / l->min_units, 4 * l->grid / std::max<int64_t>(1, hkv * groups)) +
-                         std::min(units_s, 4 * l->grid / std::max<int64_t>(1, hkv * rows));
-  l->merge_ways = 1;
-  while (l->merge_ways < 8 && pieces > 8 * l->merge_ways && (columns / 32 + 1) * hkv * 2 * l->merge_ways <= 256) l->merge_ways *= 2;
-  l->wide_slots = hkv * (columns / 32 + groups) + columns / 32 + 4 * groups + 4 * l->grid;
-  l->own_slots = hkv * rows + 4 * l->grid;
   auto align = [](size_t x) { return (x + 255) & ~(size_t)255; };
-  l->ml_wide = align(12 * sizeof(int32_t) * (size_t)rows);
+  l->ml_wide = align(sizeof(Describe) * (size_t)b->batch);
   l->o_wide = align(l->ml_wide + (size_t)l->wide_slots * 32 * 8);
   l->ml_own = align(l->o_wide + (size_t)l->wide_slots * 32 * kHeadDim * 4);
   l->o_own = align(l->ml_own + (size_t)l->own_slots * group * 8);

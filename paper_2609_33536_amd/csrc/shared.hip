@@ -41,8 +41,9 @@
 namespace ekv {
 namespace {
 
-constexpr int kWaves = 4;
-constexpr int kTileCols = kWaves * kPfCols;
+constexpr int kWaves = kSharedWaves;
+constexpr int kTileCols = kSharedTile;
+static_assert(kSharedCols == kPfCols, "a wave's columns");
 // LDS: 4 slots of K planes and 5 of V planes of a unit (tiles), or a unit's slot per wave (few, own).
 constexpr int kVSlots = 5;
 constexpr int kVRing = 4 * kPlanePf;
@@ -63,8 +64,6 @@ __device__ __forceinline__ int fresh(int lane) {
   return lane;
 }
 __device__ __forceinline__ int lane_value(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
-
-enum Kind { kNone, kFew, kTeam };
 
 // Sum over the lanes, and each lane's sum of the lanes before it.  Most launches have
 // one prefix (one lane that is not 0), which needs no scan.
@@ -95,22 +94,14 @@ struct GroupRow {
   }
 };
 
-// What follows from a prefix's sequences and length.  Its columns go to tiles of 128;
-// up to 32 of them, or up to 32 left over by the tiles, to a wave's stream (the last
-// sequences' columns: a tile's unit costs the same for one column as for 128, and
-// more than a stream's).
-struct Shape {
+// What follows from a prefix's sequences and length.
+struct Shape : ColumnSplit {
   int start, count, units, len;            // (units: 0 without any sequence)
-  int tiles, wide;                         // tiles of 128 and groups of 32 columns
-  int rest;                                // columns of the stream
   __device__ __forceinline__ Shape() {}
   __device__ __forceinline__ Shape(int start_, int end, int len_, int log2_group) : start(start_), len(len_) {
     count = len > 0 ? end - start : 0;
     units = count > 0 ? units_of(len) : 0;
-    const int columns = count << log2_group;
-    rest = columns % kTileCols <= kPfCols ? columns % kTileCols : 0;
-    tiles = (columns - rest + kTileCols - 1) / kTileCols;
-    wide = (columns - rest + kPfCols - 1) / kPfCols;
+    static_cast<ColumnSplit&>(*this) = ColumnSplit(count << log2_group);
   }
   __device__ __forceinline__ bool has(int kind) const { return kind == kTeam ? tiles > 0 : rest > 0; }
   // the first sequence of the stream's columns
@@ -133,35 +124,12 @@ struct Groups : Shape {
   }
 };
 
-// A prefix's teams: `spans` of `span` units, each cut into `cuts` runs of `run`.
-struct Teams {
-  int span, cuts, run;
-  __device__ __forceinline__ Teams(const SharedPlan& plan, int units, int hkv) {
-    span = plan.team_aligned ? units : hkv * units;
-    cuts = (span + plan.team_run - 1) / plan.team_run;
-    run = cuts > 0 ? (span + cuts - 1) / cuts : 1;
-  }
-};
-
-// Units with starts (few) or workers (team) of a prefix, and its slots (few: besides one for each worker).
-struct Amounts {
-  int work, slots;
-  __device__ __forceinline__ Amounts(const Shape& x, const SharedPlan& plan, int kind, int hkv)
-      : work(hkv * (x.units + 1)), slots(hkv) {
-    if (kind == kTeam) {
-      const Teams t(plan, x.units, hkv);
-      work = (plan.team_aligned ? hkv : 1) * t.cuts * x.tiles;
-      slots = (plan.team_aligned ? hkv * t.cuts : hkv + t.cuts) * x.wide;
-    }
-  }
-};
-
 // Where the work and the slots of 64 prefixes of one kind begin.  `work` and `slots`
 // count those before, and are advanced.
 struct Places {
   int base, end, slot;
   __device__ __forceinline__ Places(const Groups& x, const SharedPlan& plan, int kind, int hkv, int& work, int& slots) {
-    const Amounts n(x, plan, kind, hkv);
+    const Amounts n(x, x.units, plan, kind, hkv);
     const bool mine = x.has(kind);
     const LaneSum sw(mine ? n.work : 0), sn(mine ? n.slots : 0);
     base = work + sw.before;
@@ -507,16 +475,6 @@ struct Worker {
 
 // ---- what the merge is told ----------------------------------------------------
 
-// Where the pieces of a sequence's columns are: two ranges of units, the prefix's
-// (units of KV head 0's segment from `off`, `head_off` further for each head, in
-// workers of `run`; slots from `slot`, `head_slot` further for each head, `step` for
-// each worker; its columns from `col` in a slot) and its own.
-struct Describe {
-  int4 units;   // off, head_off, units, run of the prefix (run 0: none)
-  int4 slots;   // slot, head_slot, step, col
-  int4 own;     // off, units, run (0: none), 0; a head's segment is units + 1 further than the one before
-};
-
 // The prefix's part, for the sequences of chunk `chunk` (one a lane) that stand behind
 // prefix g in its columns of one kind; slot0: that kind's first slot.
 __device__ __forceinline__ void describe_prefix(Describe& d, const SharedArgs& a, const SharedPlan& plan, const Group& g, int kind,
@@ -524,15 +482,7 @@ __device__ __forceinline__ void describe_prefix(Describe& d, const SharedArgs& a
   const int s = 64 * chunk + lane, rest = g.rest_start(a.log2_group);
   const int first = kind == kFew ? rest : g.start;
   if (s < first || s >= (kind == kFew ? g.start + g.count : rest)) return;
-  const int j = (s - first) << a.log2_group, slot = slot0 + g.slot;
-  if (kind == kFew) {
-    d.units = int4{g.base + 1, g.units + 1, g.units, plan.few_run};
-    d.slots = int4{slot, 1, 1, j};
-  } else {
-    const Teams t(plan, g.units, a.num_kv_heads);
-    d.units = int4{0, plan.team_aligned ? t.cuts * t.run : g.units, g.units, t.run};
-    d.slots = int4{slot + j / kPfCols, plan.team_aligned ? 0 : g.wide, g.wide, j & (kPfCols - 1)};
-  }
+  describe_columns(d, plan, kind, a.num_kv_heads, g.units, g.wide, g.base, slot0 + g.slot, (s - first) << a.log2_group);
 }
 // Those of one kind among the 64 prefixes x whose groups reach into these sequences.
 __device__ __forceinline__ void describe_prefixes(Describe& d, const SharedArgs& a, const SharedPlan& plan, const Groups& x,
@@ -624,7 +574,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         team_units = hkv * at.tiles * at.units;
       } else {
         if (kind != kNone && at.has(kind)) {
-          at.end = Amounts(at, plan, kind, hkv).work;
+          at.end = Amounts(at, at.units, plan, kind, hkv).work;
           found = pos < at.end;
         }
         if (describes) {
@@ -666,7 +616,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     if (pass == 0) {
       plan = divide_work(SharedWork{team_units, team_tiles, hkv * team_tiles, few_work, own_work},
                          (int)gridDim.x, a.min_units, F8);
-      team_slot0 = few_segments + kWaves * plan.few_workers;
+      team_slot0 = first_team_slot(plan, few_segments);
       id = blockIdx.x;
       if (id < plan.team_workers) {
         // team workers in order of (prefix, segment, run, tile), neighbours on one XCD (ids go round robin over the 8)
@@ -709,7 +659,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         pc.u1 = min(at.units, pc.u0 + (u_end - u));
         pc.seq0 = at.start + (first >> a.log2_group);
         pc.columns = min((at.count << a.log2_group) - at.rest - first, kTileCols);
-        pc.slot = team_slot0 + at.slot + (team + (plan.team_aligned ? 0 : pc.kvh)) * at.wide + kWaves * tile;
+        pc.slot = tile_slot(plan, team_slot0 + at.slot, at.wide, team, pc.kvh, tile);
         Worker<T, ELASTIC, F8>(arguments(), ring, wave, fresh(lane)).tile(pc);
         u += pc.u1 - pc.u0;
       }
@@ -761,7 +711,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         at.units = units_of(at.len);
         at.end = at.base + hkv * (at.units + 1);
         at.rest = 1 << a.log2_group;
-        at.slot = at.p * hkv;
+        at.slot = own_slot0(at.p, hkv);
       }
       x.row = at.p;
       x.len = at.len;
@@ -774,7 +724,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
       x.u1 = min(at.units, x.u0 + min(64, u_end - u));
       x.seq0 = few ? at.rest_start(a.log2_group) : at.start;
       x.columns = at.rest;
-      x.slot = at.slot + x.kvh + id;
+      x.slot = stream_slot(at.slot, x.kvh, id);
       u += x.u1 - x.u0;
       return true;
     };
@@ -854,18 +804,13 @@ __global__ __launch_bounds__(64 * kMergeWaves) void shared_merge_kernel(SharedAr
   int wide_n = 0, wide_slot = 0, own_n = 0, own_slot = 0, step = 1, col = 0;
   if (ok) {
     const Describe d = reinterpret_cast<const Describe*>(a.plan)[s];
-    if (d.units.w > 0) {
-      const int off = d.units.x + kvh * d.units.y, w0 = off / d.units.w;
-      wide_n = (off + d.units.z - 1) / d.units.w - w0 + 1;
-      wide_slot = d.slots.x + kvh * d.slots.y + w0 * d.slots.z;
-      step = d.slots.z;
-      col = d.slots.w + head;
-    }
-    if (d.own.z > 0) {
-      const int off = d.own.x + kvh * (d.own.y + 1), w0 = off / d.own.z;
-      own_n = (off + d.own.y - 1) / d.own.z - w0 + 1;
-      own_slot = s * a.num_kv_heads + kvh + w0;
-    }
+    const PieceSlots w = prefix_pieces(d, kvh), o = own_pieces(d, s, a.num_kv_heads, kvh);
+    wide_n = w.n;
+    wide_slot = w.slot;
+    step = w.step;
+    col = d.slots.w + head;
+    own_n = o.n;
+    own_slot = o.slot;
   }
   const int all_n = wide_n + own_n;
   // this way's pieces: every `ways`-th from `way` on

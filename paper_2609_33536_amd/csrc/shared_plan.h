@@ -1,10 +1,13 @@
 // Parts of the shared-prefix decode that also compile for the host (internal
-// header): the launch's arguments, and how its workgroups are divided.
+// header): the launch's arguments and sizes, how its workgroups are divided, and
+// where the pieces' partials lie.
 #pragma once
 
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
+
+#include <algorithm>
 
 namespace ekv {
 
@@ -36,6 +39,44 @@ struct SharedArgs {
 };
 
 constexpr int kMaxSharedGrid = 512;
+constexpr int kSharedWaves = 4;                  // of a workgroup
+constexpr int kSharedCols = 32;                  // columns of a wave
+constexpr int kSharedTile = kSharedWaves * kSharedCols;
+
+// What a call is launched with, from the host's sizes alone.
+struct SharedSize {
+  int grid, min_units, merge_ways;
+  int64_t wide_slots, own_slots;   // partials of 32 columns, and of G
+};
+
+// False if the flat spaces of units do not fit 32 bits.  Slots: at most one per 32
+// columns (or part of 32) of a group and KV head, and 4 per workgroup for the segments
+// that workers cut; likewise one per sequence and KV head.
+inline bool size_shared(int64_t prefixes, int64_t rows, int64_t units_p, int64_t units_s, int64_t hkv, int64_t group,
+                        SharedSize* l) {
+  const int64_t columns = rows * group, groups = std::min<int64_t>(prefixes, rows);
+  const int64_t tiles = columns / 128 + groups;
+  const int64_t work_t = hkv * tiles * (units_p + 1), work_s = hkv * rows * (units_s + 1);   // (a segment's start counts too)
+  if (work_t >= (1 << 30) || work_s >= (1 << 30) || columns * hkv >= (1 << 30) || prefixes >= (1 << 24)) return false;
+  // The fewest units that a worker takes of a prefix, so that short prefixes leave the merge fewer
+  // pieces: with 1 instead, 64 sequences behind 2048 tokens take 27.4 us (25.3), 8 behind 8192 23.7
+  // (21.5), longer and shorter ones the same.
+  l->min_units = (int)std::max<int64_t>(1, std::min<int64_t>(4, units_p / 16));
+  const int64_t wanted = (work_t + hkv * groups * (units_p + 1) / 4 + work_s / 4) / l->min_units + 4;
+  l->grid = (int)std::min<int64_t>(kMaxSharedGrid, wanted);
+  // The merge: a workgroup takes 8 pieces a memory round trip.  Where a column may have more (at
+  // most its units, or what is left of the workers for each segment), up to 8 waves divide them, as
+  // long as the launch has at most one workgroup a compute unit.  With one wave always, 8 sequences
+  // behind 32768 tokens take 68.5 us (39.1), 4 behind 512 14.2 (12.6); with up to two workgroups a
+  // compute unit 16 prompts with samples take 66.8 (64.4).
+  const int64_t pieces = std::min(units_p / l->min_units, 4 * l->grid / std::max<int64_t>(1, hkv * groups)) +
+                         std::min(units_s, 4 * l->grid / std::max<int64_t>(1, hkv * rows));
+  l->merge_ways = 1;
+  while (l->merge_ways < 8 && pieces > 8 * l->merge_ways && (columns / 32 + 1) * hkv * 2 * l->merge_ways <= 256) l->merge_ways *= 2;
+  l->wide_slots = hkv * (columns / 32 + groups) + columns / 32 + 4 * groups + 4 * l->grid;
+  l->own_slots = hkv * rows + 4 * l->grid;
+  return true;
+}
 
 // Units (few, own: and segments) of each kind; a team's count once for each of its tiles.
 struct SharedWork {
@@ -94,6 +135,98 @@ __host__ __device__ inline SharedPlan divide_work(const SharedWork& n, int grid,
   }
   if (p.team_run < min_units) p.team_run = min_units;
   return p;
+}
+
+// ---- where the pieces are -------------------------------------------------------
+
+enum Kind { kNone, kFew, kTeam };
+
+// A prefix's columns: tiles of 128 and groups of 32 in them; up to 32 columns, or up to 32
+// left over by the tiles, to a wave's stream (the last sequences' columns: a tile's unit
+// costs the same for one column as for 128, and more than a stream's).
+struct ColumnSplit {
+  int tiles, wide, rest;
+  __host__ __device__ inline ColumnSplit() {}
+  __host__ __device__ inline explicit ColumnSplit(int columns) {
+    rest = columns % kSharedTile <= kSharedCols ? columns % kSharedTile : 0;
+    tiles = (columns - rest + kSharedTile - 1) / kSharedTile;
+    wide = (columns - rest + kSharedCols - 1) / kSharedCols;
+  }
+};
+
+// A prefix's teams: `spans` of `span` units, each cut into `cuts` runs of `run`.
+struct Teams {
+  int span, cuts, run;
+  __host__ __device__ inline Teams(const SharedPlan& plan, int units, int hkv) {
+    span = plan.team_aligned ? units : hkv * units;
+    cuts = (span + plan.team_run - 1) / plan.team_run;
+    run = cuts > 0 ? (span + cuts - 1) / cuts : 1;
+  }
+};
+
+// Units with starts (few) or workers (team) of a prefix, and its slots (few: besides one for each worker).
+struct Amounts {
+  int work, slots;
+  __host__ __device__ inline Amounts(const ColumnSplit& x, int units, const SharedPlan& plan, int kind, int hkv)
+      : work(hkv * (units + 1)), slots(hkv) {
+    if (kind == kTeam) {
+      const Teams t(plan, units, hkv);
+      work = (plan.team_aligned ? hkv : 1) * t.cuts * x.tiles;
+      slots = (plan.team_aligned ? hkv * t.cuts : hkv + t.cuts) * x.wide;
+    }
+  }
+};
+
+// The first slot of team slots (the few's come first).
+__host__ __device__ inline int first_team_slot(const SharedPlan& plan, int few_segments) {
+  return few_segments + kSharedWaves * plan.few_workers;
+}
+// A tile's piece (its first wave's; the others' follow): `slot` the prefix's first, of team `team` on KV head kvh.
+__host__ __device__ inline int tile_slot(const SharedPlan& plan, int slot, int wide, int team, int kvh, int tile) {
+  return slot + (team + (plan.team_aligned ? 0 : kvh)) * wide + kSharedWaves * tile;
+}
+// A stream's piece: `slot` the prefix's or sequence's first, `worker` the wave's number in its kind.
+__host__ __device__ inline int stream_slot(int slot, int kvh, int worker) { return slot + kvh + worker; }
+// A sequence's own first slot.
+__host__ __device__ inline int own_slot0(int sequence, int hkv) { return sequence * hkv; }
+
+// Where the pieces of a sequence's columns are, for the merge: two ranges of units, the
+// prefix's (units of KV head 0's segment from `off`, `head_off` further for each head, in
+// workers of `run`; slots from `slot`, `head_slot` further for each head, `step` for
+// each worker; its columns from `col` in a slot) and its own.
+struct Describe {
+  int4 units;   // off, head_off, units, run of the prefix (run 0: none)
+  int4 slots;   // slot, head_slot, step, col
+  int4 own;     // off, units, run (0: none), 0; a head's segment is units + 1 further than the one before
+};
+
+// The prefix's part, for a sequence whose first column is number `j` of the stream's (few) or
+// the tiles' (team); base, slot: where the prefix's units (few) and slots begin.
+__host__ __device__ inline void describe_columns(Describe& d, const SharedPlan& plan, int kind, int hkv, int units, int wide,
+                                                 int base, int slot, int j) {
+  if (kind == kFew) {
+    d.units = int4{base + 1, units + 1, units, plan.few_run};
+    d.slots = int4{slot, 1, 1, j};
+  } else {
+    const Teams t(plan, units, hkv);
+    d.units = int4{0, plan.team_aligned ? t.cuts * t.run : units, units, t.run};
+    d.slots = int4{slot + j / kSharedCols, plan.team_aligned ? 0 : wide, wide, j & (kSharedCols - 1)};
+  }
+}
+
+// Pieces of one KV head: `n` of them, at slot, slot + step, ...
+struct PieceSlots {
+  int n, slot, step;
+};
+__host__ __device__ inline PieceSlots prefix_pieces(const Describe& d, int kvh) {
+  if (d.units.w <= 0) return PieceSlots{0, 0, 1};
+  const int off = d.units.x + kvh * d.units.y, w0 = off / d.units.w;
+  return PieceSlots{(off + d.units.z - 1) / d.units.w - w0 + 1, d.slots.x + kvh * d.slots.y + w0 * d.slots.z, d.slots.z};
+}
+__host__ __device__ inline PieceSlots own_pieces(const Describe& d, int sequence, int hkv, int kvh) {
+  if (d.own.z <= 0) return PieceSlots{0, 0, 1};
+  const int off = d.own.x + kvh * (d.own.y + 1), w0 = off / d.own.z;
+  return PieceSlots{(off + d.own.y - 1) / d.own.z - w0 + 1, stream_slot(own_slot0(sequence, hkv), kvh, w0), 1};
 }
 
 // Workgroups resident on the current device.

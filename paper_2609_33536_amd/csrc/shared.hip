@@ -21,10 +21,10 @@
 //   own    a sequence's own tokens, G columns: likewise.
 // The workgroups are divided between the kinds by the work that each has.  The units of
 // few and own are one flat space each, in which a segment's start counts as a unit; a
-// wave takes an equal run of it and crosses segments;
-// a team stays in one segment where that costs little (a start costs as much as 5
-// units), else it crosses the KV heads of its prefix.  Piece k of a segment is therefore
-// made by worker w_first + k, and its slot of partials follows from segment and worker.
+// wave takes an equal run of it and crosses segments; a team stays in one segment where
+// that makes its run little longer (divide_work), else it crosses the KV heads of its
+// prefix.  Piece k of a segment is therefore made by worker w_first + k, and its slot of
+// partials follows from segment and worker.
 //
 // What bounds it: behind a prefix of many columns matrix work (256 sequences of 64 query
 // heads behind 32768 tokens: 0.93 PFLOP/s with P's remainder, a plain product reaches 1.22),

@@ -109,6 +109,9 @@ __host__ __device__ inline SharedPlan divide_work(const SharedWork& n, int grid,
   // Two tiles on one compute unit run slower than a tile beside streams: a few tiles more
   // than compute units are not worth it (three 8-bit prefixes of 16384 tokens and 55
   // sequences of up to 2048: 91.9 us, with the 273 tile workers of the weights alone 97.8).
+  // Of 257 to 282 such tiles holding back was 2 to 12 % faster (6 of 6 batches), at 310 to 318
+  // between 9 % faster (launches of 25 to 31 us) and 6 % slower (139 us); of more,
+  // launches under 32 us would still gain 4 to 14 %, those of 100 us and more lose 4 to 23 %.
   constexpr int cus = kMaxSharedGrid / 2;
   const bool whole = t > cus && 4 * t < 5 * cus && f + o > 0;
   if (whole) t = cus;
@@ -125,9 +128,13 @@ __host__ __device__ inline SharedPlan divide_work(const SharedWork& n, int grid,
     // every prefix (or segment) rounds its number of teams up, which adds at most its tiles
     const int half = (t + 1) / 2, free = t - n.team_tiles > half ? t - n.team_tiles : half;
     p.team_run = (n.team_units + free - 1) / free;
+    // One segment a team, unless that makes the run more than 5 units longer.  Over batches of 1
+    // and 3 prefixes, runs up to 4 units longer were 0.4 to 12 % faster than shorter ones across
+    // segments (12 of 12); 6 to 10 longer 1.5 % slower with 8-bit pools (7 of 10), and alike with
+    // 16-bit ones (10 instead of 5 there: 0.98 to 1.035 of the time where it changes anything).
     if (t > n.team_segments) {
       const int run = (n.team_units + t - n.team_segments - 1) / (t - n.team_segments);
-      if (run <= p.team_run + 5) {   // (a start costs a worker what 5 units do)
+      if (run <= p.team_run + 5) {
         p.team_run = run;
         p.team_aligned = 1;
       }

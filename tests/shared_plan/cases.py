@@ -14,9 +14,9 @@ def _own(n, most, seed, **at):
 # name: (query heads, KV heads, prefix lengths, group boundaries, own lengths, sequences to compare, what the division is)
 CASES = {
     # few workers for each segment: a team's run goes on in the next KV head, its rings used again
-    "teams-cross-heads": (64, 4, [4100], [0, 256], _own(256, 40, 1), [0, 9, 130, 255],
-                          "not team_aligned and 129 % team_run != 0"),
-    "teams-cross-heads-of-two-prefixes": (64, 4, [3000, 2100], [1, 140, 262], _own(263, 40, 2), [0, 1, 100, 139, 140, 261, 262],
+    "teams-cross-heads": (64, 4, [6200], [0, 256], _own(256, 40, 1), [0, 9, 130, 255],
+                          "not team_aligned and 194 % team_run != 0"),
+    "teams-cross-heads-of-two-prefixes": (64, 4, [5200, 4100], [1, 140, 262], _own(263, 40, 2), [0, 1, 100, 139, 140, 261, 262],
                                           "not team_aligned"),
     # more tiles than workers: they come round again
     "tiles-in-rounds": (16, 1, [33 + p % 7 for p in range(600)], list(range(0, 4801, 8)), _own(4800, 20, 3),

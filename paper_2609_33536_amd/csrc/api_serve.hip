@@ -117,8 +117,8 @@ ekv_status debug_check_free(const ExtendArgs& a, hipStream_t stream, const char*
   const auto twice = std::adjacent_find(open.begin(), open.end());
   if (twice != open.end()) return fail(EKV_ERR_INVALID, "%s (EKV_DEBUG): block %d is in the free list twice", call, *twice);
   for (int s = 0; s < a.batch; ++s) {
-    const int len = (int)std::min<int64_t>(std::max(lens[s], 0), (int64_t)a.max_blocks * kPage);
-    for (int b = 0; b < (len + kPage - 1) / kPage; ++b) {
+    if (lens[s] < 0 || lens[s] > (int64_t)a.max_blocks * kPage) continue;   // (the call's status says so)
+    for (int b = 0; b < (lens[s] + kPage - 1) / kPage; ++b) {
       const int32_t id = table[(size_t)s * a.max_blocks + b];
       if (std::binary_search(open.begin(), open.end(), id))
         return fail(EKV_ERR_INVALID, "%s (EKV_DEBUG): block %d is free and held by sequence %d", call, id, s);

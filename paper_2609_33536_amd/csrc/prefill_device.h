@@ -152,27 +152,8 @@ struct Stager {
     dst = (row >> 2) * kGroup + 256 * (chunk >> 1) + 64 * (row & 3) + 32 * (chunk & 1);
     v_off = (uint64_t)num_kv_heads * kTileP;
   }
-  // Quarter q of a unit, tile: the K tile of the quarter's block (a BASE
-  // pair's: the packed tile), slot: the unit's slot (LDS address).
-  __device__ __forceinline__ void load(uint64_t tile, bool base, int q, uint32_t slot) const {
-    const uint32_t to = slot + quarter_offset(q);
-    const uint64_t packed = tile + (uint32_t)(q >> 1) * (kTileP / 2);
-    if constexpr (F8) {
-      const uint32_t off = base ? src_n : src_b;
-      const uint64_t src = base ? packed + (q & 1) * 8 * (kHeadDim / 2) : tile + (q & 1) * 8 * kHeadDim;
-      dma16(src, off, to);
-      dma16(src + v_off, off, to + kPlanePf);
-    } else {
-      const uint32_t off = base ? src_b : src_t;
-      const uint64_t src = base ? packed + (q & 1) * 8 * kHeadDim : tile + (q & 1) * 8 * 2 * kHeadDim;
-      const uint64_t src2 = src + (base ? 0 : 1024);
-      dma16(src, off, to);
-      dma16(src2, off, to + kGroup);
-      dma16(src + v_off, off, to + kPlanePf);
-      dma16(src2 + v_off, off, to + kPlanePf + kGroup);
-    }
-  }
-  // The two planes of a quarter to places of their own (K first: kLoads / 2 loads each).
+  // Quarter q of a unit, its two planes to places of their own (K first: kLoads / 2 loads
+  // each).  tile: the K tile of the quarter's block (a BASE pair's: the packed tile).
   __device__ __forceinline__ void load_planes(uint64_t tile, bool base, int q, uint32_t k_slot, uint32_t v_slot) const {
     const uint32_t at = quarter_offset(q);
     const uint64_t packed = tile + (uint32_t)(q >> 1) * (kTileP / 2);
@@ -191,8 +172,12 @@ struct Stager {
       dma16(src2 + v_off, off, v_slot + at + kGroup);
     }
   }
-  // As widen, for one plane's slot, in two steps: what landed, and its words in place
-  // (by one wave, which reads all of its quarter before it writes).
+  // ... to the unit's slot (LDS address).
+  __device__ __forceinline__ void load(uint64_t tile, bool base, int q, uint32_t slot) const {
+    load_planes(tile, base, q, slot, slot + kPlanePf);
+  }
+  // After quarter q of a plane has landed: what landed, and bytes or nibbles -> words in
+  // place (by one wave, all of whose reads precede its writes).
   __device__ __forceinline__ u32x4 landed_plane(const char* slot, bool base, int q, int lane) const {
     const char* at = slot + quarter_offset(q);
     if (!F8 && !base) return u32x4{0u, 0u, 0u, 0u};
@@ -212,6 +197,8 @@ struct Stager {
     *reinterpret_cast<u32x4*>(at + dst) = expand_base8(raw.xy);
     *reinterpret_cast<u32x4*>(at + dst + 16) = expand_base8(raw.zw);
   }
+  // Zero V rows for keys at or past `valid` (their slots may hold anything, and 0 * NaN
+  // would poison the products).  key0: the unit's first key.
   __device__ __forceinline__ void clear_tail(char* v_slot, int q, int key0, int valid) const {
     if (key0 + 2 * kPage > valid && key0 + 8 * q + row >= valid) {
       char* at = v_slot + quarter_offset(q) + dst;
@@ -219,10 +206,8 @@ struct Stager {
       *reinterpret_cast<u32x4*>(at + 16) = u32x4{0u, 0u, 0u, 0u};
     }
   }
-  // After quarter q has landed: bytes or nibbles -> words in place (every
-  // lane's reads precede the wave's writes), and zero V rows for keys at or
-  // past `valid` (their slots may hold anything, and 0 * NaN would poison
-  // the products).  key0: the unit's first key.
+  // Both planes of quarter q of a unit's slot, in one step: under one branch where the two
+  // functions above take one each (prefill's code grows by 0.7 % with them).
   __device__ __forceinline__ void widen(char* slot, bool base, int q, int key0, int valid, int lane) const {
     char* at = slot + quarter_offset(q);
     if (F8 || base) {
@@ -243,10 +228,7 @@ struct Stager {
         *reinterpret_cast<u32x4*>(at + pl * kPlanePf + dst + 16) = expand_base8(raw[pl].zw);
       }
     }
-    if (key0 + 2 * kPage > valid && key0 + 8 * q + row >= valid) {
-      *reinterpret_cast<u32x4*>(at + kPlanePf + dst) = u32x4{0u, 0u, 0u, 0u};
-      *reinterpret_cast<u32x4*>(at + kPlanePf + dst + 16) = u32x4{0u, 0u, 0u, 0u};
-    }
+    clear_tail(slot + kPlanePf, q, key0, valid);
   }
 };
 

@@ -13,8 +13,9 @@
 // binary search in the sums.  Nothing is passed between workgroups.  Lengths and
 // cursor may be updated in place: one workgroup does so behind a barrier; of
 // several, all of which read them, none may, and a second launch of one does.
-// Bound by latency: 64 single tokens 4.0 us (an empty launch takes 4.1 back to back),
-// 192 sequences with 24 thousand tokens 4.8, 512 prompts with 538 thousand 7.1.
+// Bound by latency: 64 single tokens 4.1 us (an empty launch takes as long back to back),
+// 192 sequences with 24 thousand tokens 4.8, 512 prompts with 538 thousand 7.2; in place
+// 3.7, 7.4 and 10.2.
 #include "common.h"
 #include "extend.h"
 #include "wave_scan.h"
@@ -136,7 +137,7 @@ __global__ __launch_bounds__(kThreads) void extend_kernel(ExtendArgs a) {
       }
     }
     // ---- tokens: one a thread where there are threads for all of them (4096 sequences of one
-    // token: 12.1 us, four neighbours a thread 15.4)
+    // token: 11.9 us, four neighbours a thread 15.4)
     if (a.max_tokens <= step) {
       if (first < a.max_tokens) {
         int slot = -1, pos = 0;
@@ -220,9 +221,9 @@ __global__ __launch_bounds__(kThreads) void extend_kernel(ExtendArgs a) {
 }  // namespace
 
 hipError_t launch_extend(const ExtendArgs& a, hipStream_t st) {
-  // One token a thread up to three workgroups a CU (48 KB of LDS each; 538 thousand tokens: 7.1 us,
-  // with 512 and 256 workgroups 8.9 and 10.7).  In place, one workgroup does for 2048
-  // tokens: 5.3 us, where 8 take 3.9 and the second launch as much again.
+  // One token a thread up to three workgroups a CU (48 KB of LDS each; 538 thousand tokens: 7.2 us,
+  // with 512 and 256 workgroups 9.0 and 11.1).  In place, one workgroup does for 2048
+  // tokens: 4.8 us, where 8 and the second launch take 5.6 (512 tokens: 3.7 and 5.1).
   const bool in_place = a.lens_out == a.lens || a.cursor_out == a.cursor;
   const int64_t work = a.max_tokens > a.batch ? a.max_tokens : a.batch;
   int64_t grid = (work + kThreads - 1) / kThreads;

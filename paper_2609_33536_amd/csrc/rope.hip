@@ -12,8 +12,8 @@
 // elements 8c.. and rotary_dim / 2 + 8c..; pair layout: 16c .. 16c + 15), so that a
 // lane's cosines and sines serve every head that its wave turns.  The kernel is bound
 // by HBM: q in and out, k and v in, their cache rows out.  16384 tokens of 64 + 2 x 8 heads
-// into an 8-bit pool take 127 us (638 MB, 5.0 TB/s; a plain copy reaches 5.2), 64 tokens of
-// 32 + 2 x 8 heads 4.2 us (a launch).
+// into an 8-bit pool, not in a cache, take 128 us (638 MB, 5.0 TB/s; a plain copy reaches
+// 5.2), 64 tokens of 32 + 2 x 8 heads 4.4 us (a launch).
 #include <algorithm>
 
 #include "common.h"
@@ -197,8 +197,8 @@ hipError_t launch_rope(const RopeArgs& a, int dtype, hipStream_t st) {
   const int rows = a.num_q_heads + 2 * a.num_kv_heads;
   // A wave works the angles out once for its rows, 8 at a time: as many rows as leave 2048
   // waves (8 a CU).  Measured with 48 rows a token, us at 8 / 16 / 24 / 48 rows a wave:
-  // 64 tokens 4.2 / 4.6 / 5.0 / 6.5, 512 tokens 6.3 / 5.6 / 6.0 / 7.2, 1024 tokens
-  // 8.5 / 7.2 / 7.0 / 7.8, 8192 tokens 47.8 / 35.5 / 33.8 / 34.6.
+  // 64 tokens 4.4 / 4.8 / 5.3 / 6.7, 512 tokens 6.1 / 5.7 / 6.1 / 7.4, 1024 tokens
+  // 9.2 / 7.5 / 7.0 / 7.9, 8192 tokens 52.1 / 41.2 / 38.5 / 37.6.
   const int64_t share = ((int64_t)a.n * rows + 2047) / 2048;
   b.rows_per_wave = (int)std::min<int64_t>((share + 7) / 8 * 8, rows);
   const int64_t waves = (int64_t)a.n * ((rows + b.rows_per_wave - 1) / b.rows_per_wave);   // (at most 2048 + a.n)

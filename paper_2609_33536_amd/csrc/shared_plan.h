@@ -96,7 +96,7 @@ struct SharedPlan {
 // segment costs its start (table, queries, first loads) and its partials: one unit of
 // a wave's stream, and of a tile 5, or 10 where first loads queue behind streams that
 // use all of HBM's rate (16-bit pools: 64 sequences of up to 2048 behind 64 tokens
-// 95.9 us at 5, 84.5 at 10; 8-bit, 55 of up to 2048 behind 256 tokens 41.0 and 48.4).
+// 95.9 us at 5, 84.5 at 10; 8-bit, 44 of up to 2048 behind 256 tokens 41.0 and 48.4).
 __host__ __device__ inline SharedPlan divide_work(const SharedWork& n, int grid, int min_units, bool bytes8) {
   const float stream = bytes8 ? 1.75f : 2.5f;
   const float team = 4.f * n.team_units + (bytes8 ? 20.f : 40.f) * n.team_segments;
@@ -107,7 +107,7 @@ __host__ __device__ inline SharedPlan divide_work(const SharedWork& n, int grid,
   if (n.few_work > 0 && f == 0) f = 1;
   if (n.own_work > 0 && o == 0) o = 1;
   // Two tiles on one compute unit run slower than a tile beside streams: a few tiles more
-  // than compute units are not worth it (three 8-bit prefixes of 16384 tokens and 55
+  // than compute units are not worth it (three 8-bit prefixes of 16384 tokens and 44
   // sequences of up to 2048: 91.9 us, with the 273 tile workers of the weights alone 97.8).
   // Of 257 to 282 such tiles holding back was 2 to 12 % faster (6 of 6 batches), at 310 to 318
   // between 9 % faster (launches of 25 to 31 us) and 6 % slower (139 us); of more,

@@ -30,7 +30,8 @@
 // heads behind 32768 tokens: 0.94 PFLOP/s with P's remainder, a plain product reaches 1.22),
 // otherwise HBM (64 sequences of 32 heads behind 8192 tokens, repeated: 187 MB in 39 us, 9
 // of them before the stream is up, and 6 for the merge; 8 more on inputs in no cache);
-// 8-bit pools the chain of a unit (widening, softmax, products).  64 sequences of 8192 tokens each in rows of their own take 316 us.
+// 8-bit pools the chain of a unit (widening, softmax, products).  64 sequences of 8192
+// tokens each in rows of their own take 316 us.
 #include <algorithm>
 #include <atomic>
 

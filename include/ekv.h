@@ -442,12 +442,12 @@ ekv_status ekv_check_transition(int32_t kind, const int32_t* h_pairs, int32_t n,
  * Asynchronous on the stream; nothing else is written.
  *
  * With EKV_DEBUG=1 in the environment, ekv_attn_decode, ekv_attn_prefill,
- * ekv_attn_decode_shared (for its prefixes and its batch) and every transition
- * call run these checks first, synchronise the stream, and return
+ * ekv_attn_decode_shared (for its prefixes and its batch), ekv_key_bounds,
+ * ekv_select_blocks, ekv_attn_decode_selected and every transition call run these checks first, synchronise the stream, and return
  * EKV_ERR_INVALID (naming the first violation) without enqueuing anything
  * else; so do ekv_extend for a free list that names a block twice, or one
- * that a sequence of the table holds, and ekv_rope_append for a slot given to
- * two rows (both copy these arrays to the host and check them there).
+ * that a sequence of the table holds, and ekv_rope_append and
+ * ekv_norm_rope_append for a slot given to two rows (both copy these arrays to the host and check them there).
  * The checks above report into a static 96-byte device
  * array of the library (one per device; calls in this mode from several
  * host threads on one device race on it) and is meant for debugging only.
@@ -704,6 +704,34 @@ ekv_status ekv_rope_append(const ekv_pool* pool, const ekv_rope* rope, int32_t n
                            hipStream_t stream);
 
 /*
+ * Norms of query and key heads, for models that level each head before its
+ * rotation: element i of a head x becomes
+ *   x_i / sqrt(mean(x^2) + eps) * (offset + weight_i)
+ */
+typedef struct {
+  const void* q_weight;   /* device [128] of the query dtype for each head, q_stride values apart, 16-byte aligned; or NULL: factor 1 */
+  const void* k_weight;   /* the same for key heads */
+  int32_t q_stride;       /* 0 (one weight for all heads), or a multiple of 8 from 128 on */
+  int32_t k_stride;
+  float eps;              /* from 1e-30 to 1e6 */
+  float offset;           /* 0, or 1 for models that store their weights less one */
+} ekv_head_norm;
+
+/*
+ * ekv_rope_append with each query and key head levelled by `norm` first, in the
+ * same pass: norm, weight and rotation in 32 bits, rounded once.  Elements behind
+ * rotary_dim are levelled too; values are stored as they come.  A head whose
+ * squares overflow 32 bits is levelled all the same.  Other arguments as
+ * ekv_rope_append.
+ * Errors: as ekv_rope_append; EKV_ERR_INVALID also for a NULL norm, weight
+ * strides, alignment, eps and offset.
+ */
+ekv_status ekv_norm_rope_append(const ekv_pool* pool, const ekv_rope* rope, const ekv_head_norm* norm, int32_t n,
+                                const int32_t* positions, const int32_t* slots, const void* q, int64_t q_stride,
+                                int32_t num_q_heads, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                                void* q_out, int64_t q_out_stride, hipStream_t stream);
+
+/*
  * Decode attention over shared prefixes, one query token per sequence.
  * `prefixes` describes the prefixes as `batch` does the sequences: a row of
  * its table, tags and lengths per prefix, its own mode, the same
@@ -737,6 +765,88 @@ size_t ekv_decode_shared_workspace_bytes(const ekv_pool* pool, const ekv_batch* 
 ekv_status ekv_attn_decode_shared(const ekv_pool* pool, const ekv_batch* prefixes, const int32_t* group_start,
                                   const ekv_batch* batch, const void* q, void* out, int32_t out_dtype, float scale,
                                   void* ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * ---- Long contexts ----------------------------------------------------------
+ *
+ * A decode step that reads a part of a long context: bounds of each block's keys,
+ * kept as the cache grows (ekv_key_bounds); the blocks whose bounds allow the
+ * largest scores against a step's queries (ekv_select_blocks); attention over those
+ * alone (ekv_attn_decode_selected).  Per step and layer: ekv_extend,
+ * ekv_rope_append or ekv_norm_rope_append, then these three.  All of them can be captured in a
+ * HIP graph and replayed.
+ */
+
+/*
+ * Bounds of the keys of each block, for every KV head and channel the smallest
+ * and the largest executed key (each block read in its mode, as ekv_attn_decode)
+ * over the tokens that the sequence has in the block:
+ *   bounds  device [batch][num_kv_heads][max_blocks][2][head_dim], element type of
+ *           the pool (bytes for an 8-bit one), 16-byte aligned; [0] smallest,
+ *           [1] largest; a row per row of the batch, by logical block, so that
+ *           transitions and the free list need not know of it
+ *   known   device int32 [batch]: tokens of each sequence whose bounds are there
+ *           already, i.e. its length before the new tokens; NULL: none
+ * Logical blocks known[s] / page_size to the last with tokens are written, the
+ * others left as they were.  Nothing is rounded.  -0 is below 0; a NaN lies beyond the infinity of its
+ * sign, so it shows in its bound.  A transition changes the executed values of its
+ * pairs: a later call with known[s] at or before them refreshes the bounds.  (Bounds
+ * from before it only make the scores of those blocks less tight or less sure.)
+ * Errors: as ekv_attn_decode; EKV_ERR_UNSUPPORTED also for more than 2^22 rows (batch
+ * times KV heads).
+ */
+ekv_status ekv_key_bounds(const ekv_pool* pool, const ekv_batch* batch, const int32_t* known, void* bounds,
+                          hipStream_t stream);
+
+/*
+ * The blocks that a decode step reads.  For sequence s and KV head h, with the G
+ * query heads g of h, block i has the score
+ *   sum_c (sum_g max(q_gc, 0)) hi_ic + (sum_g min(q_gc, 0)) lo_ic
+ * which no key of the block exceeds in sum_g q_g . k.  It is computed in 64 bits.  Of
+ * the n blocks that hold tokens, the first `sink` and the last `recent` are taken, and of the others
+ * those with the largest scores (the lowest block first among equals; a score that is
+ * not a number is the largest), min(n, budget) in all.  (A negative softmax scale turns
+ * the order of scores round; it is not known here.)
+ *   q         device [batch][num_q_heads][head_dim], query dtype (the pool's, or FP16
+ *             for an 8-bit pool)
+ *   bounds    as ekv_key_bounds writes them
+ *   selected  device int32 [batch][num_kv_heads][budget]: the logical blocks in
+ *             ascending order, then -1
+ *   counts    device int32 [batch][num_kv_heads]: min(n, budget)
+ *   ws        device scratch of ekv_select_workspace_bytes() bytes, 16-byte aligned,
+ *             prepared by ekv_decode_workspace_init (or zero-filled) before its first
+ *             use; calls that share one must be ordered
+ * 0 <= sink, recent; sink + recent <= budget < 2^20.  Of the pool only its shape and of the
+ * batch its lengths and sizes are used.
+ * Errors: as ekv_key_bounds; EKV_ERR_INVALID also for the budget, sink and recent, and
+ * the workspace.  ekv_select_workspace_bytes returns 0 for shapes that are refused.
+ */
+size_t ekv_select_workspace_bytes(const ekv_pool* pool, const ekv_batch* batch, int32_t budget);
+ekv_status ekv_select_blocks(const ekv_pool* pool, const ekv_batch* batch, const void* q, const void* bounds, int32_t budget,
+                             int32_t sink, int32_t recent, int32_t* selected, int32_t* counts, void* ws, size_t ws_bytes,
+                             hipStream_t stream);
+
+/*
+ * Decode attention over selected blocks, one query token per sequence: as
+ * ekv_attn_decode, but for sequence s and KV head h over the tokens of the logical
+ * blocks selected[s][h][0 .. counts[s][h]) alone (of the block that the sequence
+ * ends in, those it has).
+ *   selected  device int32 [batch][num_kv_heads][budget]; entries that are no block of
+ *             the sequence (-1, say) are passed over; a block must not be listed twice
+ *             (it would count twice).  Any order; ascending is as ekv_select_blocks leaves them
+ *   counts    device int32 [batch][num_kv_heads], clamped into [0, budget]; NULL: budget
+ *   ws        device scratch of ekv_decode_selected_workspace_bytes() bytes, 16-byte
+ *             aligned, prepared by ekv_decode_workspace_init (or zero-filled) before
+ *             its first use; it may be used with other batches; calls that share one
+ *             must be ordered
+ * A head without a token yields zeros.  q, out and the pool are 16-byte aligned.
+ * Errors: as ekv_key_bounds; EKV_ERR_INVALID also for out_dtype, scale, budget and the
+ * workspace; with EKV_DEBUG=1 for a block that is listed twice.
+ */
+size_t ekv_decode_selected_workspace_bytes(const ekv_pool* pool, const ekv_batch* batch, int32_t budget);
+ekv_status ekv_attn_decode_selected(const ekv_pool* pool, const ekv_batch* batch, const int32_t* selected,
+                                    const int32_t* counts, int32_t budget, const void* q, void* out, int32_t out_dtype,
+                                    float scale, void* ws, size_t ws_bytes, hipStream_t stream);
 
 #ifdef __cplusplus
 }

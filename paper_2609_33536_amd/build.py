@@ -18,8 +18,8 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libekv.so")
 TIMELINE_LIB = os.path.join(HERE, "libekv_timeline.so")
-SOURCES = ["api.hip", "api_serve.hip", "control.hip", "decode.hip", "extend.hip", "prefill.hip", "rope.hip", "shared.hip",
-           "transition.hip", "validate.hip"]
+SOURCES = ["api.hip", "api_context.hip", "api_serve.hip", "control.hip", "decode.hip", "decode_selected.hip", "extend.hip",
+           "key_bounds.hip", "prefill.hip", "rope.hip", "select.hip", "shared.hip", "transition.hip", "validate.hip"]
 ARCH = "gfx950"
 
 FLAGS = [

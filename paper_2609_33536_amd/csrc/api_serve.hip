@@ -17,6 +17,9 @@ namespace {
 
 using namespace ekv;
 
+// (squares too small for 32 bits do not count beside the least eps, the most does not beside squares too large)
+constexpr float kLeastEps = 1e-30f, kMostEps = 1e6f;
+
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
 // ---- shared-prefix decode -------------------------------------------------
@@ -127,6 +130,77 @@ ekv_status debug_check_free(const ExtendArgs& a, hipStream_t stream, const char*
   return EKV_OK;
 }
 
+// ---- rotary append, with or without the norms -----------------------------
+
+ekv_status check_norm(const ekv_head_norm* norm) {
+  if (!(norm->eps >= kLeastEps && norm->eps <= kMostEps)) return fail(EKV_ERR_INVALID, "eps must be from 1e-30 to 1e6");
+  if (!std::isfinite(norm->offset)) return fail(EKV_ERR_INVALID, "offset must be finite");
+  for (const int32_t stride : {norm->q_stride, norm->k_stride})
+    if ((stride != 0 && stride < kHeadDim) || stride % 8 || stride >= (1 << 20))
+      return fail(EKV_ERR_INVALID, "a weight stride must be 0 or a multiple of 8 from 128 to 2^20");
+  if (!aligned16(norm->q_weight) || !aligned16(norm->k_weight))
+    return fail(EKV_ERR_INVALID, "weights must be 16-byte aligned");
+  return EKV_OK;
+}
+
+// norm: NULL for ekv_rope_append.  `call` and `launch` name the entry point in messages.
+ekv_status rope_append(const char* call, const char* launch, const ekv_pool* pool, const ekv_rope* rope,
+                       const ekv_head_norm* norm, int32_t n, const int32_t* positions, const int32_t* slots, const void* q,
+                       int64_t q_stride, int32_t num_q_heads, const void* k, int64_t k_stride, const void* v,
+                       int64_t v_stride, void* q_out, int64_t q_out_stride, hipStream_t stream) {
+  ekv_status st = check_pool(pool);
+  if (st != EKV_OK) return st;
+  if (!rope || !rope->turns) return fail(EKV_ERR_INVALID, "rope and its turns are required");
+  if (rope->rotary_dim <= 0 || rope->rotary_dim % 16 || rope->rotary_dim > kHeadDim)
+    return fail(EKV_ERR_UNSUPPORTED, "rotary_dim must be a multiple of 16, at most 128");
+  if (rope->layout != EKV_ROPE_HALF && rope->layout != EKV_ROPE_PAIRS)
+    return fail(EKV_ERR_INVALID, "unknown rotary layout %d", rope->layout);
+  if (!std::isfinite(rope->magnitude)) return fail(EKV_ERR_INVALID, "magnitude must be finite");
+  if (norm && (st = check_norm(norm)) != EKV_OK) return st;
+  if (n < 0 || num_q_heads <= 0) return fail(EKV_ERR_INVALID, "bad sizes");
+  if (n >= (1 << 26) || num_q_heads > 1024) return fail(EKV_ERR_UNSUPPORTED, "at most 2^26 tokens and 1024 query heads");
+  if (n == 0) return EKV_OK;
+  if (!positions || !slots || !q || !k || !v || !q_out)
+    return fail(EKV_ERR_INVALID, "positions, slots, q, k, v and q_out are required");
+  const int64_t q_row = (int64_t)num_q_heads * kHeadDim, kv_row = (int64_t)pool->num_kv_heads * kHeadDim;
+  if (q_stride < q_row || q_out_stride < q_row || k_stride < kv_row || v_stride < kv_row)
+    return fail(EKV_ERR_INVALID, "a row stride is shorter than its heads");
+  if ((q_stride | q_out_stride | k_stride | v_stride) % 8 || !aligned16(q) || !aligned16(k) || !aligned16(v) ||
+      !aligned16(q_out) || !aligned16(pool->kv))
+    return fail(EKV_ERR_INVALID, "rows must be 16-byte aligned");
+  if (debug_mode() && (st = debug_check_slots(pool, n, slots, stream, call)) != EKV_OK) return st;
+  RopeArgs a{};
+  a.positions = positions;
+  a.slots = slots;
+  a.q = static_cast<const uint16_t*>(q);
+  a.k = static_cast<const uint16_t*>(k);
+  a.v = static_cast<const uint16_t*>(v);
+  a.q_out = static_cast<uint16_t*>(q_out);
+  a.pool = pool->kv;
+  a.turns = rope->turns;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.out_stride = q_out_stride;
+  a.n = n;
+  a.num_q_heads = num_q_heads;
+  a.num_kv_heads = pool->num_kv_heads;
+  a.num_blocks = pool->num_blocks;
+  a.rotary_dim = rope->rotary_dim;
+  a.pairs = rope->layout == EKV_ROPE_PAIRS;
+  a.magnitude = rope->magnitude;
+  if (norm) {
+    a.norm = 1;
+    a.q_weight = static_cast<const uint16_t*>(norm->q_weight);
+    a.k_weight = static_cast<const uint16_t*>(norm->k_weight);
+    a.q_weight_stride = norm->q_stride;
+    a.k_weight_stride = norm->k_stride;
+    a.eps = norm->eps;
+    a.offset = norm->offset;
+  }
+  return hip_status(launch_rope(a, pool->dtype, stream), launch);
+}
+
 }  // namespace
 
 extern "C" {
@@ -206,47 +280,19 @@ ekv_status ekv_rope_append(const ekv_pool* pool, const ekv_rope* rope, int32_t n
                            int64_t k_stride, const void* v, int64_t v_stride, void* q_out, int64_t q_out_stride,
                            hipStream_t stream) {
   return ekv::guard("ekv_rope_append", [&]() -> ekv_status {
-    ekv_status st = check_pool(pool);
-    if (st != EKV_OK) return st;
-    if (!rope || !rope->turns) return fail(EKV_ERR_INVALID, "rope and its turns are required");
-    if (rope->rotary_dim <= 0 || rope->rotary_dim % 16 || rope->rotary_dim > kHeadDim)
-      return fail(EKV_ERR_UNSUPPORTED, "rotary_dim must be a multiple of 16, at most 128");
-    if (rope->layout != EKV_ROPE_HALF && rope->layout != EKV_ROPE_PAIRS)
-      return fail(EKV_ERR_INVALID, "unknown rotary layout %d", rope->layout);
-    if (!std::isfinite(rope->magnitude)) return fail(EKV_ERR_INVALID, "magnitude must be finite");
-    if (n < 0 || num_q_heads <= 0) return fail(EKV_ERR_INVALID, "bad sizes");
-    if (n >= (1 << 26) || num_q_heads > 1024) return fail(EKV_ERR_UNSUPPORTED, "at most 2^26 tokens and 1024 query heads");
-    if (n == 0) return EKV_OK;
-    if (!positions || !slots || !q || !k || !v || !q_out)
-      return fail(EKV_ERR_INVALID, "positions, slots, q, k, v and q_out are required");
-    const int64_t q_row = (int64_t)num_q_heads * kHeadDim, kv_row = (int64_t)pool->num_kv_heads * kHeadDim;
-    if (q_stride < q_row || q_out_stride < q_row || k_stride < kv_row || v_stride < kv_row)
-      return fail(EKV_ERR_INVALID, "a row stride is shorter than its heads");
-    if ((q_stride | q_out_stride | k_stride | v_stride) % 8 || !aligned16(q) || !aligned16(k) || !aligned16(v) ||
-        !aligned16(q_out) || !aligned16(pool->kv))
-      return fail(EKV_ERR_INVALID, "rows must be 16-byte aligned");
-    if (debug_mode() && (st = debug_check_slots(pool, n, slots, stream, "ekv_rope_append")) != EKV_OK) return st;
-    RopeArgs a{};
-    a.positions = positions;
-    a.slots = slots;
-    a.q = static_cast<const uint16_t*>(q);
-    a.k = static_cast<const uint16_t*>(k);
-    a.v = static_cast<const uint16_t*>(v);
-    a.q_out = static_cast<uint16_t*>(q_out);
-    a.pool = pool->kv;
-    a.turns = rope->turns;
-    a.q_stride = q_stride;
-    a.k_stride = k_stride;
-    a.v_stride = v_stride;
-    a.out_stride = q_out_stride;
-    a.n = n;
-    a.num_q_heads = num_q_heads;
-    a.num_kv_heads = pool->num_kv_heads;
-    a.num_blocks = pool->num_blocks;
-    a.rotary_dim = rope->rotary_dim;
-    a.pairs = rope->layout == EKV_ROPE_PAIRS;
-    a.magnitude = rope->magnitude;
-    return hip_status(launch_rope(a, pool->dtype, stream), "ekv_rope_append launch");
+    return rope_append("ekv_rope_append", "ekv_rope_append launch", pool, rope, nullptr, n, positions, slots, q, q_stride,
+                       num_q_heads, k, k_stride, v, v_stride, q_out, q_out_stride, stream);
+  });
+}
+
+ekv_status ekv_norm_rope_append(const ekv_pool* pool, const ekv_rope* rope, const ekv_head_norm* norm, int32_t n,
+                                const int32_t* positions, const int32_t* slots, const void* q, int64_t q_stride,
+                                int32_t num_q_heads, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                                void* q_out, int64_t q_out_stride, hipStream_t stream) {
+  return ekv::guard("ekv_norm_rope_append", [&]() -> ekv_status {
+    if (!norm) return fail(EKV_ERR_INVALID, "norm is NULL");
+    return rope_append("ekv_norm_rope_append", "ekv_norm_rope_append launch", pool, rope, norm, n, positions, slots, q,
+                       q_stride, num_q_heads, k, k_stride, v, v_stride, q_out, q_out_stride, stream);
   });
 }
 

@@ -21,6 +21,12 @@ struct RopeArgs {
   int32_t pairs;             // pair i: elements (2i, 2i + 1) rather than (i, i + rotary_dim / 2)
   float magnitude;
   int32_t rows_per_wave;     // set by the launcher
+  // The norm of each query and key head (norm = 0: none, the rest is not read)
+  int32_t norm;
+  const uint16_t* q_weight;  // [128] a head, `*_weight_stride` values apart (0: one for all heads), or null (ones)
+  const uint16_t* k_weight;
+  int32_t q_weight_stride, k_weight_stride;
+  float eps, offset;         // inside the root; added to the weights
 };
 
 // dtype: of the pool (0 bf16, 1 fp16, 3 8-bit with FP16 inputs)

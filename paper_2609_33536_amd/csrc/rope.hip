@@ -86,8 +86,52 @@ __device__ __forceinline__ void floats8(u32x4 w, float (&x)[8]) {
   }
 }
 
-// ONCE: inputs are read past the caches
-template <typename T, bool F8, bool ONCE>
+// Sum over the 8 lanes that hold a head (each pair, each four, then the other four, mirrored).
+__device__ __forceinline__ float sum8(float x) {
+  x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0xB1, 0xf, 0xf, true));    // quad_perm 1,0,3,2
+  x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x4E, 0xf, 0xf, true));    // quad_perm 2,3,0,1
+  x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x141, 0xf, 0xf, true));   // row_half_mirror
+  return x;
+}
+__device__ __forceinline__ float squares(const float (&x)[8], const float (&y)[8]) {
+  float s = 0.0f, t = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    s = fmaf(x[i], x[i], s);
+    t = fmaf(y[i], y[i], t);
+  }
+  return sum8(s + t);
+}
+
+// A head's elements times 1 / sqrt(mean of their squares + eps) and the weights.  Squares
+// are summed in 32 bits; where that overflows (bf16 values beyond 10^18), over elements
+// 2^-70 as large, whose squares are far above any eps that was not lost before.
+template <typename T>
+__device__ __forceinline__ void level(const RopeArgs& a, float (&x)[8], float (&y)[8], bool weighted, u32x4 w0, u32x4 w1) {
+  constexpr float kDown = 0x1p-70f;
+  float sum = squares(x, y), eps = a.eps;
+  if (!(sum < __builtin_inff())) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      x[i] *= kDown;
+      y[i] *= kDown;
+    }
+    sum = squares(x, y);
+    eps = 0.0f;
+  }
+  const float f = __builtin_amdgcn_rsqf(fmaf(sum, 1.0f / kHeadDim, eps));
+  float u[8], v[8];
+  floats8<T>(w0, u);
+  floats8<T>(w1, v);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    x[i] *= weighted ? f * (u[i] + a.offset) : f;
+    y[i] *= weighted ? f * (v[i] + a.offset) : f;
+  }
+}
+
+// ONCE: inputs are read past the caches.  NORM: query and key heads are levelled first
+template <typename T, bool F8, bool ONCE, bool NORM>
 __global__ __launch_bounds__(64 * kWaves) void rope_kernel(RopeArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 7;
   const int rows = a.num_q_heads + 2 * a.num_kv_heads;   // rows of a token: query heads, key heads, value heads
@@ -103,6 +147,14 @@ __global__ __launch_bounds__(64 * kWaves) void rope_kernel(RopeArgs a) {
   const int chunk0 = a.pairs ? 2 * c : (c < turned ? c : 2 * turned + 2 * (c - turned));
   const int chunk1 = a.pairs ? 2 * c + 1 : (c < turned ? turned + c : chunk0 + 1);
   const int values0 = a.num_q_heads + a.num_kv_heads;              // the first value head
+  auto load_weights = [&](int r, u32x4& w0, u32x4& w1) {   // (the same few rows for every token: from the caches)
+    const bool key = r >= a.num_q_heads;
+    const uint16_t* src = key ? a.k_weight : a.q_weight;
+    if (!src || r >= values0) return;
+    src += key ? (r - a.num_q_heads) * a.k_weight_stride : r * a.q_weight_stride;
+    w0 = *reinterpret_cast<const u32x4*>(src + 8 * chunk0);
+    w1 = *reinterpret_cast<const u32x4*>(src + 8 * chunk1);
+  };
   auto load = [&](int r, u32x4& w0, u32x4& w1) {
     const uint16_t* src = r < a.num_q_heads ? a.q + token * a.q_stride + (size_t)r * kHeadDim
                           : r < values0     ? a.k + token * a.k_stride + (size_t)(r - a.num_q_heads) * kHeadDim
@@ -119,7 +171,11 @@ __global__ __launch_bounds__(64 * kWaves) void rope_kernel(RopeArgs a) {
   // (the first row's values are on their way while the angles are worked out, the next row's while one is turned)
   int r = row0 + (lane >> 3);
   u32x4 next0{0u, 0u, 0u, 0u}, next1{0u, 0u, 0u, 0u};
-  if (r < row_end) load(r, next0, next1);
+  u32x4 weight0{0u, 0u, 0u, 0u}, weight1{0u, 0u, 0u, 0u};
+  if (r < row_end) {
+    load(r, next0, next1);
+    if constexpr (NORM) load_weights(r, weight0, weight1);
+  }
 
   const bool in_pool = slot >= 0 && slot / kPage < a.num_blocks;   // (outside the pool: the cache is left as it is)
   float cs[8], sn[8];
@@ -133,14 +189,21 @@ __global__ __launch_bounds__(64 * kWaves) void rope_kernel(RopeArgs a) {
 #pragma unroll 1
   for (; r < row_end; r += 8) {
     u32x4 w0 = next0, w1 = next1;
-    if (r + 8 < row_end) load(r + 8, next0, next1);
+    const u32x4 u0 = weight0, u1 = weight1;
+    if (r + 8 < row_end) {
+      load(r + 8, next0, next1);
+      if constexpr (NORM) load_weights(r + 8, weight0, weight1);
+    }
     const int kind = r < a.num_q_heads ? 0 : (r < values0 ? 1 : 2);   // query, key, value
     if (kind != 0 && !in_pool) continue;
     float x[8], y[8];
-    if (kind != 2 && c < turned) {
+    if (kind != 2 && (NORM || c < turned)) {
       floats8<T>(w0, x);
       floats8<T>(w1, y);
-      if (a.pairs) {   // elements 16 c + 2 i, + 1
+      if constexpr (NORM) level<T>(a, x, y, (kind == 0 ? a.q_weight : a.k_weight) != nullptr, u0, u1);
+      if (NORM && c >= turned) {
+        // (levelled, not turned)
+      } else if (a.pairs) {   // elements 16 c + 2 i, + 1
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float x0 = x[2 * i], x1 = x[2 * i + 1], y0 = y[2 * i], y1 = y[2 * i + 1];
@@ -183,10 +246,15 @@ __global__ __launch_bounds__(64 * kWaves) void rope_kernel(RopeArgs a) {
   }
 }
 
+template <typename T, bool F8, bool NORM>
+void launch_once(const RopeArgs& a, dim3 grid, dim3 block, bool once, hipStream_t st) {
+  if (once) hipLaunchKernelGGL((rope_kernel<T, F8, true, NORM>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((rope_kernel<T, F8, false, NORM>), grid, block, 0, st, a);
+}
 template <typename T, bool F8>
 void launch_typed(const RopeArgs& a, dim3 grid, dim3 block, bool once, hipStream_t st) {
-  if (once) hipLaunchKernelGGL((rope_kernel<T, F8, true>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((rope_kernel<T, F8, false>), grid, block, 0, st, a);
+  if (a.norm) launch_once<T, F8, true>(a, grid, block, once, st);
+  else launch_once<T, F8, false>(a, grid, block, once, st);
 }
 
 }  // namespace

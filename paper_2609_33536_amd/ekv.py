@@ -51,6 +51,11 @@ class Rope(ctypes.Structure):
                 ("magnitude", ctypes.c_float)]
 
 
+class HeadNorm(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("q_stride", ctypes.c_int32),
+                ("k_stride", ctypes.c_int32), ("eps", ctypes.c_float), ("offset", ctypes.c_float)]
+
+
 class CtrlConfig(ctypes.Structure):
     _fields_ = [("min_batch", ctypes.c_int32), ("decay", ctypes.c_int32), ("a_max", ctypes.c_int32),
                 ("sink_pairs", ctypes.c_int32), ("recent_pairs", ctypes.c_int32), ("policy", ctypes.c_int32),
@@ -112,9 +117,16 @@ SIGNATURES = {
     "ekv_rope_freqs": (_I, [_I, _D, _I, _D, _D, _D, _D, _P]),
     "ekv_rope_append": (_I, [ctypes.POINTER(Pool), ctypes.POINTER(Rope), _I, _P, _P, _P, _L, _I, _P, _L, _P, _L, _P,
                              _L, _S]),
+    "ekv_norm_rope_append": (_I, [ctypes.POINTER(Pool), ctypes.POINTER(Rope), ctypes.POINTER(HeadNorm), _I, _P, _P, _P, _L,
+                                  _I, _P, _L, _P, _L, _P, _L, _S]),
     "ekv_decode_shared_workspace_bytes": (_U, [ctypes.POINTER(Pool), ctypes.POINTER(Batch), ctypes.POINTER(Batch)]),
     "ekv_attn_decode_shared": (_I, [ctypes.POINTER(Pool), ctypes.POINTER(Batch), _P, ctypes.POINTER(Batch), _P, _P, _I,
                                     _F, _P, _U, _S]),
+    "ekv_key_bounds": (_I, [ctypes.POINTER(Pool), ctypes.POINTER(Batch), _P, _P, _S]),
+    "ekv_select_workspace_bytes": (_U, [ctypes.POINTER(Pool), ctypes.POINTER(Batch), _I]),
+    "ekv_select_blocks": (_I, [ctypes.POINTER(Pool), ctypes.POINTER(Batch), _P, _P, _I, _I, _I, _P, _P, _P, _U, _S]),
+    "ekv_decode_selected_workspace_bytes": (_U, [ctypes.POINTER(Pool), ctypes.POINTER(Batch), _I]),
+    "ekv_attn_decode_selected": (_I, [ctypes.POINTER(Pool), ctypes.POINTER(Batch), _P, _P, _I, _P, _P, _I, _F, _P, _U, _S]),
 }
 
 _lib = None
@@ -518,17 +530,49 @@ def _rows(t, shape, dtype, name):
     return t.data_ptr(), row if shape[0] > 1 else shape[1] * HEAD_DIM
 
 
-def rope_append(pool, rope, positions, slots, q, k, v, q_out, stream=None):
-    """ekv_rope_append: q, q_out [n][Hq][128] and k, v [n][Hkv][128] may be
-    views of wider rows (the heads of a row packed)."""
+def _rope_arguments(pool, positions, slots, q, k, v, q_out):
     import torch
     n, hq, hkv = q.shape[0], q.shape[1], pool.num_kv_heads
     dtype = torch.bfloat16 if pool.dtype == DTYPE_BF16 else torch.float16
     (qp, qs), (op, os_) = _rows(q, (n, hq, HEAD_DIM), dtype, "q"), _rows(q_out, (n, hq, HEAD_DIM), dtype, "q_out")
     (kp, ks), (vp, vs) = _rows(k, (n, hkv, HEAD_DIM), dtype, "k"), _rows(v, (n, hkv, HEAD_DIM), dtype, "v")
-    _check(lib().ekv_rope_append(ctypes.byref(pool), ctypes.byref(rope), n, _typed(positions, torch.int32, (n,), "positions"),
-                                 _typed(slots, torch.int32, (n,), "slots"), qp, qs, hq, kp, ks, vp, vs, op, os_,
-                                 _stream(stream)))
+    return (n, _typed(positions, torch.int32, (n,), "positions"), _typed(slots, torch.int32, (n,), "slots"), qp, qs, hq, kp,
+            ks, vp, vs, op, os_)
+
+
+def rope_append(pool, rope, positions, slots, q, k, v, q_out, stream=None):
+    """ekv_rope_append: q, q_out [n][Hq][128] and k, v [n][Hkv][128] may be
+    views of wider rows (the heads of a row packed)."""
+    _check(lib().ekv_rope_append(ctypes.byref(pool), ctypes.byref(rope),
+                                 *_rope_arguments(pool, positions, slots, q, k, v, q_out), _stream(stream)))
+
+
+def _head_weight(t, name):
+    """(pointer, stride between heads) of the weight [128] of all heads or [heads][128] of each."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda or t.dim() not in (1, 2) or t.shape[-1] != HEAD_DIM or not t.is_contiguous():
+        raise EkvError(ERR_INVALID, f"{name} must be a contiguous GPU tensor [128] or [heads][128]")
+    return t.data_ptr(), 0 if t.dim() == 1 else HEAD_DIM
+
+
+def make_head_norm(q_weight=None, k_weight=None, eps=1e-6, offset=0.0):
+    """Describe the norms of query and key heads: weights of the query dtype,
+    [128] for all heads or [heads][128] for each, or None (ones)."""
+    (qp, qs), (kp, ks) = _head_weight(q_weight, "q_weight"), _head_weight(k_weight, "k_weight")
+    norm = HeadNorm(qp, kp, qs, ks, eps, offset)
+    norm.tensors = (q_weight, k_weight)   # (kept: the struct holds their addresses)
+    return norm
+
+
+def norm_rope_append(pool, rope, norm, positions, slots, q, k, v, q_out, stream=None):
+    """ekv_norm_rope_append: :func:`rope_append` with every query and key head
+    levelled first (:func:`make_head_norm`)."""
+    for weight, x, name in zip(getattr(norm, "tensors", (None, None)), (q, k), ("q_weight", "k_weight")):
+        if weight is not None and (weight.dtype is not x.dtype or (weight.dim() == 2 and weight.shape[0] != x.shape[1])):
+            raise EkvError(ERR_INVALID, f"{name} must be {x.dtype} [128] or [{x.shape[1]}][128]")
+    _check(lib().ekv_norm_rope_append(ctypes.byref(pool), ctypes.byref(rope), ctypes.byref(norm),
+                                      *_rope_arguments(pool, positions, slots, q, k, v, q_out), _stream(stream)))
 
 
 def decode_shared_workspace_bytes(pool, prefixes, batch):
@@ -556,3 +600,92 @@ def attn_decode_shared(pool, prefixes, group_start, batch, q, out, scale, ws, st
     _check(lib().ekv_attn_decode_shared(ctypes.byref(pool), ctypes.byref(prefixes), start,
                                         ctypes.byref(batch), qp, op, dtype_code(out.dtype), scale, _ptr(ws),
                                         ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def _query_type(pool):
+    import torch
+    return torch.bfloat16 if pool.dtype == DTYPE_BF16 else torch.float16
+
+
+def _bounds_ptr(pool, batch, bounds):
+    """Device pointer of bounds [batch][Hkv][max_blocks][2][128] of the pool's element type (or words of its size)."""
+    import torch
+    kinds = {DTYPE_BF16: (torch.bfloat16, torch.int16), DTYPE_FP16: (torch.float16, torch.int16),
+             DTYPE_E5M2: (torch.float8_e5m2, torch.uint8)}[pool.dtype]
+    shape = (batch.batch, pool.num_kv_heads, batch.max_blocks, 2, HEAD_DIM)
+    if bounds is None or bounds.dtype not in kinds or bounds.shape != shape:
+        raise EkvError(ERR_INVALID, f"bounds must be {kinds[0]} or {kinds[1]} {shape}")
+    return _ptr(bounds)
+
+
+def key_bounds_buffer(pool, batch, device="cuda"):
+    """An array for :func:`key_bounds`, words (bytes for an 8-bit pool) of zeros."""
+    import torch
+    return torch.zeros((batch.batch, pool.num_kv_heads, batch.max_blocks, 2, HEAD_DIM),
+                       dtype=torch.uint8 if pool.dtype == DTYPE_E5M2 else torch.int16, device=device)
+
+
+def key_bounds(pool, batch, bounds, known=None, stream=None):
+    """ekv_key_bounds: the smallest and largest keys of the blocks from
+    known[s] / 16 on (int32 [batch]: tokens whose bounds are there; None: all)."""
+    import torch
+    _check(lib().ekv_key_bounds(ctypes.byref(pool), ctypes.byref(batch), _typed(known, torch.int32, (batch.batch,), "known"),
+                                _bounds_ptr(pool, batch, bounds), _stream(stream)))
+
+
+def _workspace(nbytes, device):
+    import torch
+    if nbytes == 0:
+        raise EkvError(ERR_INVALID, lib().ekv_last_error().decode())
+    return torch.zeros(nbytes, dtype=torch.uint8, device=device)
+
+
+def select_workspace_bytes(pool, batch, budget):
+    return lib().ekv_select_workspace_bytes(ctypes.byref(pool), ctypes.byref(batch), int(budget))
+
+
+def select_workspace(pool, batch, budget, device="cuda"):
+    """A zero-filled workspace for :func:`select_blocks`."""
+    return _workspace(select_workspace_bytes(pool, batch, budget), device)
+
+
+def select_blocks(pool, batch, q, bounds, selected, counts, ws, sink=1, recent=1, stream=None):
+    """ekv_select_blocks: the blocks of the largest scores, into selected int32
+    [batch][Hkv][budget] and counts int32 [batch][Hkv]; the first `sink` and the
+    last `recent` blocks are always taken."""
+    import torch
+    rows = (batch.batch, pool.num_kv_heads)
+    if selected is None or selected.dim() != 3:
+        raise EkvError(ERR_INVALID, "selected must be int32 [batch][num_kv_heads][budget]")
+    budget = selected.shape[2]
+    _check(lib().ekv_select_blocks(ctypes.byref(pool), ctypes.byref(batch),
+                                   _typed(q, _query_type(pool), (batch.batch, batch.num_q_heads, HEAD_DIM), "q"),
+                                   _bounds_ptr(pool, batch, bounds), budget, sink, recent,
+                                   _typed(selected, torch.int32, (*rows, budget), "selected"),
+                                   _typed(counts, torch.int32, rows, "counts"), _ptr(ws), ws.numel() * ws.element_size(),
+                                   _stream(stream)))
+
+
+def decode_selected_workspace_bytes(pool, batch, budget):
+    return lib().ekv_decode_selected_workspace_bytes(ctypes.byref(pool), ctypes.byref(batch), int(budget))
+
+
+def decode_selected_workspace(pool, batch, budget, device="cuda"):
+    """A zero-filled workspace for :func:`attn_decode_selected` (its merge counters start at zero)."""
+    return _workspace(decode_selected_workspace_bytes(pool, batch, budget), device)
+
+
+def attn_decode_selected(pool, batch, selected, counts, q, out, scale, ws, stream=None):
+    """Decode over the blocks selected int32 [batch][Hkv][budget], counts int32
+    [batch][Hkv] of them (None: all; entries that are no block are passed over)."""
+    import torch
+    if selected is None or selected.dim() != 3 or q is None or out is None:
+        raise EkvError(ERR_INVALID, "selected [batch][num_kv_heads][budget], q and out are required")
+    rows, shape, dtype = (batch.batch, pool.num_kv_heads), (batch.batch, batch.num_q_heads, HEAD_DIM), _query_type(pool)
+    budget = selected.shape[2]
+    _check(lib().ekv_attn_decode_selected(ctypes.byref(pool), ctypes.byref(batch),
+                                          _typed(selected, torch.int32, (*rows, budget), "selected"),
+                                          _typed(counts, torch.int32, rows, "counts"), budget, _typed(q, dtype, shape, "q"),
+                                          _typed(out, torch.float32 if out.dtype is torch.float32 else dtype, shape, "out"),
+                                          dtype_code(out.dtype), scale, _ptr(ws), ws.numel() * ws.element_size(),
+                                          _stream(stream)))

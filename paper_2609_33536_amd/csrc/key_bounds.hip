@@ -9,8 +9,6 @@
 // in the upper bits of such integers, with whatever lies below them left in place (it only decides between equals).
 //
 // It is bound by HBM: 4 KiB of keys read and 512 bytes written a block and head (16-bit TARGET).
-// A wave's loads depend on its table entries, one round trip a pair; up to 32 waves a compute
-// unit, 8 KiB each, cover that.
 #include <algorithm>
 
 #include "common.h"
@@ -31,26 +29,20 @@ __device__ __forceinline__ uint32_t low2(uint32_t a, uint32_t b) {
 __device__ __forceinline__ uint32_t high2(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(s16x2, a), __builtin_bit_cast(s16x2, b)));
 }
-// The ordered form of two words, and back; of bytes and nibbles: BITS below the sign of each element.
+// The ordered form of two words (bytes: in their upper halves), and back; of 8 nibbles.
 __device__ __forceinline__ uint32_t turn_words(uint32_t w, uint32_t mask) {
   return w ^ (__builtin_bit_cast(uint32_t, __builtin_bit_cast(s16x2, w) >> 15) & mask);
 }
-__device__ __forceinline__ uint32_t turn_bytes(uint32_t w) {
-  const uint32_t sign = (w >> 7) & 0x01010101u;
-  return w ^ ((sign << 7) - sign);
-}
 __device__ __forceinline__ uint32_t turn_nibbles(uint32_t w) {
   const uint32_t sign = (w >> 3) & 0x11111111u;
-  return w ^ ((sign << 3) - sign);
+  uint32_t up = sign << 3;
+  asm("" : "+v"(up));   // (else the two become a multiplication, four times as slow as both)
+  return w ^ (up - sign);
 }
 template <int N>
 __device__ __forceinline__ uint32_t up(uint32_t w) {
   return __builtin_bit_cast(uint32_t, (u16x2)(__builtin_bit_cast(u16x2, w) << (unsigned short)N));
 }
-
-struct Extremes {
-  uint32_t low[4], high[4];   // 8 channels, two a register
-};
 
 // The 16-bit elements of a row that a lane holds, in ordered form, 8 in all: words as they lie;
 // bytes (2 registers) as elements (0, 2), (1, 3), (4, 6), (5, 7); nibbles (1) as (0, 4), (1, 5), (2, 6), (3, 7).
@@ -62,11 +54,10 @@ __device__ __forceinline__ void ordered(u32x4 w, uint32_t (&x)[4]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = turn_words(w[i], 0x7FFF7FFFu);
   } else if constexpr (FORM == kBytes) {
-    const uint32_t a = turn_bytes(w[0]), b = turn_bytes(w[1]);
-    x[0] = up<8>(a);
-    x[1] = a;
-    x[2] = up<8>(b);
-    x[3] = b;
+    x[0] = turn_words(up<8>(w[0]), 0x7FFF7FFFu);
+    x[1] = turn_words(w[0], 0x7FFF7FFFu);
+    x[2] = turn_words(up<8>(w[1]), 0x7FFF7FFFu);
+    x[3] = turn_words(w[1], 0x7FFF7FFFu);
   } else {
     const uint32_t a = turn_nibbles(w[0]);
     x[0] = up<12>(a);
@@ -76,181 +67,277 @@ __device__ __forceinline__ void ordered(u32x4 w, uint32_t (&x)[4]) {
   }
 }
 
-// Back to 8 executed words in the order of the elements.
-template <int FORM>
-__device__ __forceinline__ u32x4 executed(const uint32_t (&x)[4]) {
+// Four registers of extremes, joined over the lanes that hold the same channels (l, l ^ 16, l ^ 32, l ^ 48) and dealt out
+// to them: row group r of lanes gets elements 2 r, 2 r + 1, as executed words.
+template <int FORM, bool HIGH>
+__device__ __forceinline__ uint32_t joined(const uint32_t (&x)[4]) {
+  constexpr uint32_t kLow = 0x05040100u, kUp = 0x07060302u;   // (both low halves), (both high halves)
+  uint32_t y[4];
   if constexpr (FORM == kWords) {
-    u32x4 w;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = turn_words(x[i], 0x7FFF7FFFu);
-    return w;
+    for (int i = 0; i < 4; ++i) y[i] = x[i];
+  } else if constexpr (FORM == kBytes) {
+    y[0] = perm(x[1], x[0], kLow);
+    y[1] = perm(x[1], x[0], kUp);
+    y[2] = perm(x[3], x[2], kLow);
+    y[3] = perm(x[3], x[2], kUp);
   } else {
-    constexpr uint32_t kKeep = FORM == kBytes ? 0xFF00FF00u : 0xF000F000u, kMask = FORM == kBytes ? 0x7F007F00u : 0x70007000u;
-    uint32_t y[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = turn_words(x[i] & kKeep, kMask);
-    constexpr uint32_t kLow = 0x05040100u, kHigh = 0x07060302u;   // (both low halves), (both high halves)
-    if constexpr (FORM == kBytes) return u32x4{perm(y[1], y[0], kLow), perm(y[1], y[0], kHigh), perm(y[3], y[2], kLow), perm(y[3], y[2], kHigh)};
-    else return u32x4{perm(y[1], y[0], kLow), perm(y[3], y[2], kLow), perm(y[1], y[0], kHigh), perm(y[3], y[2], kHigh)};
+    y[0] = perm(x[1], x[0], kLow);
+    y[1] = perm(x[3], x[2], kLow);
+    y[2] = perm(x[1], x[0], kUp);
+    y[3] = perm(x[3], x[2], kUp);
   }
+  auto pick = [](uint32_t a, uint32_t b) { return HIGH ? high2(a, b) : low2(a, b); };
+  const auto a = __builtin_amdgcn_permlane16_swap(y[0], y[1], false, false);
+  const auto b = __builtin_amdgcn_permlane16_swap(y[2], y[3], false, false);
+  const auto c = __builtin_amdgcn_permlane32_swap(pick(a[0], a[1]), pick(b[0], b[1]), false, false);
+  constexpr uint32_t kKeep = FORM == kWords ? 0xFFFFFFFFu : (FORM == kBytes ? 0xFF00FF00u : 0xF000F000u);
+  return turn_words(pick(c[0], c[1]) & kKeep, kKeep & 0x7FFF7FFFu);
 }
 
-// min or max over the four lanes that hold the same channels (l, l ^ 16, l ^ 32, l ^ 48)
-template <bool HIGH>
-__device__ __forceinline__ uint32_t joined(uint32_t x) {
-  const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-  const uint32_t y = HIGH ? high2(a[0], a[1]) : low2(a[0], a[1]);
-  const auto b = __builtin_amdgcn_permlane32_swap(y, y, false, false);
-  return HIGH ? high2(b[0], b[1]) : low2(b[0], b[1]);
-}
+// What a lane loads of a row: its 8 channels as words (16 bytes), or bytes (8).  Of a BASE row, half as wide, it
+// loads as much, at a multiple of that, and takes its half: the number of loads in flight does
+// not depend on the mode, so waits count them exactly.
+template <bool F8> struct Lane;
+template <> struct Lane<false> {
+  typedef u32x4 row;
+  static __device__ __forceinline__ u32x4 base(u32x4 w, bool odd) { return u32x4{odd ? w.z : w.x, odd ? w.w : w.y, 0u, 0u}; }
+  static __device__ __forceinline__ u32x4 target(u32x4 w) { return w; }
+};
+template <> struct Lane<true> {
+  typedef u32x2 row;
+  static __device__ __forceinline__ u32x4 base(u32x2 w, bool odd) { return u32x4{odd ? w.y : w.x, 0u, 0u, 0u}; }
+  static __device__ __forceinline__ u32x4 target(u32x2 w) { return u32x4{w.x, w.y, 0u, 0u}; }
+};
 
-// A lane's 8 channels of row 4 r + lane / 16 of a tile whose rows are `row` bytes.
-template <int FORM>
-__device__ __forceinline__ void load_rows(const char* tile, int lane, u32x4 (&w)[4]) {
-  constexpr int kRow = FORM == kWords ? 2 * kHeadDim : (FORM == kBytes ? kHeadDim : kHeadDim / 2);
-  const char* p = tile + (lane >> 4) * kRow + (lane & 15) * (kRow / 16);
+// The bounds of the `live` first rows: lane (r, l) = (lane / 16, lane % 16) gets elements 8 l + 2 r, + 1, as executed words.
+template <int FORM, bool F8>
+__device__ __forceinline__ void reduce(const typename Lane<F8>::row (&w)[4], int live, int lane, uint32_t& low, uint32_t& high) {
+  constexpr bool kTarget = FORM == (F8 ? kBytes : kWords);
+  uint32_t x[4][4];
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    const char* at = p + 4 * r * kRow;
-    if constexpr (FORM == kWords) w[r] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(at));
-    else if constexpr (FORM == kBytes) w[r].xy = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(at));
-    else w[r].x = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(at));
-  }
-}
-
-// The bounds of the `live` first rows, as executed words: the smallest in lanes of even row groups, the largest in odd ones.
-template <int FORM>
-__device__ __forceinline__ u32x4 reduce(const u32x4 (&w)[4], int live, int lane) {
-  Extremes e;
+  for (int r = 0; r < 4; ++r) ordered<FORM>(kTarget ? Lane<F8>::target(w[r]) : Lane<F8>::base(w[r], lane & 1), x[r]);
+  uint32_t lo[4], hi[4];
+  if (live == kPage) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    e.low[i] = 0x7FFF7FFFu;
-    e.high[i] = 0x80008000u;
-  }
+    for (int i = 0; i < 4; ++i) {
+      lo[i] = low2(low2(x[0][i], x[1][i]), low2(x[2][i], x[3][i]));
+      hi[i] = high2(high2(x[0][i], x[1][i]), high2(x[2][i], x[3][i]));
+    }
+  } else {
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    uint32_t x[4];
-    ordered<FORM>(w[r], x);
-    if (live == kPage) {
+    for (int i = 0; i < 4; ++i) {
+      lo[i] = 0x7FFF7FFFu;
+      hi[i] = 0x80008000u;
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const bool counts = 4 * r + (lane >> 4) < live;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        e.low[i] = low2(e.low[i], x[i]);
-        e.high[i] = high2(e.high[i], x[i]);
-      }
-    } else if (4 * r + (lane >> 4) < live) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        e.low[i] = low2(e.low[i], x[i]);
-        e.high[i] = high2(e.high[i], x[i]);
+        lo[i] = low2(lo[i], counts ? x[r][i] : 0x7FFF7FFFu);
+        hi[i] = high2(hi[i], counts ? x[r][i] : 0x80008000u);
       }
     }
   }
-  uint32_t out[4];
-  const bool high = lane & 16;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t a = joined<false>(e.low[i]), b = joined<true>(e.high[i]);
-    out[i] = high ? b : a;
-  }
-  return executed<FORM>(out);
+  low = joined<FORM, false>(lo);
+  high = joined<FORM, true>(hi);
 }
 
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }   // (the same in all lanes)
 __device__ __forceinline__ int clamped(int x, int lo, int hi) { return x < lo ? lo : (x > hi ? hi : x); }
 
-// Wave w takes the w-th equal share of the units: (sequence, KV head, pair of blocks with at least one
-// changed block), in this order.
+// Wave w takes the w-th equal share of the units: (sequence, pair of blocks with at least one changed
+// block, KV head), in this order, so that a pair's table entries serve all heads and its tiles lie side by side.  A
+// unit's loads go out before the one before it is reduced.
 template <bool F8, bool ELASTIC>
 __global__ __launch_bounds__(64 * kWaves) void key_bounds_kernel(BoundsArgs a) {
   constexpr int kTile = F8 ? kTileBytes / 2 : kTileBytes, kElem = F8 ? 1 : 2;
+  typedef typename Lane<F8>::row Row;
   const BlockRows& b = a.rows;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int hkv = b.num_kv_heads;
-  auto length = [&](int s) { return s < b.batch ? clamped(b.lens[s], 0, b.len_cap) : 0; };
-  auto first_block = [&](int s) { return a.known && s < b.batch ? max(a.known[s], 0) / kPage : 0; };
-  auto pairs = [&](int s) {   // with a changed block
-    const int blocks = (length(s) + kPage - 1) / kPage, from = first_block(s);
-    return from < blocks ? (blocks + 1) / 2 - from / 2 : 0;
+  // Lane l: length and first changed block of sequence window + l.
+  int window = 0, len_lane = 0, from_lane = 0;
+  auto read_lengths = [&](int c0) {
+    window = c0;
+    len_lane = from_lane = 0;
+    if (c0 + lane < b.batch) {
+      const int length = b.lens[c0 + lane], known = (a.known ? a.known : b.lens)[c0 + lane];   // (one round trip)
+      len_lane = clamped(length, 0, b.len_cap);
+      from_lane = a.known ? max(known, 0) / kPage : 0;
+    }
   };
-  int mine = 0;
+  auto pairs_lane = [&]() {   // with a changed block
+    const int blocks = (len_lane + kPage - 1) / kPage;
+    return from_lane < blocks ? (blocks + 1) / 2 - from_lane / 2 : 0;
+  };
+  read_lengths(0);
+  int mine = pairs_lane();
+  const int first_pairs = mine;
 #pragma unroll 1
-  for (int s = lane; s < b.batch; s += 64) mine += pairs(s);
-  const int64_t units = (int64_t)last_lane(sum_scan(mine)) * hkv, waves = (int64_t)gridDim.x * kWaves;
-  const int64_t id = (int64_t)blockIdx.x * kWaves + wave;
-  int64_t u = units * id / waves;
-  const int64_t end = units * (id + 1) / waves;
-  if (u >= end) return;
+  for (int c0 = 64; c0 < b.batch; c0 += 64) {
+    read_lengths(c0);
+    mine += pairs_lane();
+  }
+  const uint32_t units = (uint32_t)last_lane(sum_scan(mine)) * hkv, waves = gridDim.x * kWaves, id = blockIdx.x * kWaves + wave;
+  const uint32_t share = units / waves, extra = units - share * waves;   // (the first `extra` waves take one more)
+  const uint32_t begin = id * share + min(id, extra), end = begin + share + (id < extra ? 1 : 0);
+  if (begin >= end) return;
 
-  // the sequence of unit u
-  int s = 0, np = 0;
-  int64_t seq = 0;   // its first unit
+  // A sequence, and the position in it of the unit whose loads go out next.
+  int s = 0, np = 0, j = 0, kvh = 0, len = 0, from = 0;
   {
-    int cum = 0;
+    uint32_t cum = 0;
 #pragma unroll 1
     for (int c0 = 0;; c0 += 64) {
-      const int x = pairs(c0 + lane), incl = sum_scan(x);
-      const uint64_t hit = __builtin_amdgcn_ballot_w64((int64_t)(cum + incl) * hkv > u);
+      if (c0 != window) read_lengths(c0);
+      const int x = c0 == 0 ? first_pairs : pairs_lane(), incl = sum_scan(x);
+      const uint64_t hit = __builtin_amdgcn_ballot_w64((cum + incl) * hkv > begin);
       if (hit) {
         const int l = __builtin_ctzll(hit);
-        s = c0 + l;
+        s = uniform(c0 + l);
         np = __builtin_amdgcn_readlane(x, l);
-        seq = (int64_t)(cum + __builtin_amdgcn_readlane(incl, l) - np) * hkv;
+        const uint32_t off = begin - (cum + __builtin_amdgcn_readlane(incl, l) - np) * hkv;
+        j = uniform(off / hkv);
+        kvh = uniform(off - j * hkv);
         break;
       }
       cum += last_lane(incl);
     }
   }
-  int kvh = (int)((u - seq) / np), j = (int)(u - seq) - kvh * np;
-
-  while (true) {
-    const int len = length(s), from = first_block(s), blocks = (len + kPage - 1) / kPage;
-    int base_lo = 0, base_hi = 0;
-    bool by_tags = ELASTIC && b.tags;
-    if (ELASTIC && b.base && b.base[2 * s] >= 0) {
-      by_tags = false;
-      base_lo = 2 * b.base[2 * s];
-      base_hi = 2 * b.base[2 * s + 1];
-    }
-    for (; kvh < hkv; ++kvh, j = 0) {
-      for (; j < np; ++j) {
-        // both blocks' loads first, then both reductions
-        const int i0 = 2 * (from / 2 + j);
-        u32x4 w[2][4];
-        bool base[2], changed[2];
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-          const int i = i0 + m;
-          changed[m] = i >= from && i < blocks;
-          base[m] = false;
-          if (!changed[m]) continue;
-          const size_t at = (size_t)s * b.max_blocks + i;
-          const int entry = b.bt[at], phys = (unsigned)entry < (unsigned)b.num_blocks ? entry : 0;   // never leave the pool
-          if constexpr (ELASTIC) base[m] = by_tags ? b.tags[at] != 0 : (i >= base_lo && i < base_hi);
-          const char* tile = reinterpret_cast<const char*>(b.pool) + ((size_t)phys * 2 * hkv + kvh) * kTile;
-          if (base[m]) load_rows<F8 ? kNibbles : kBytes>(tile + m * (kTile / 2), lane, w[m]);
-          else load_rows<F8 ? kBytes : kWords>(tile, lane, w[m]);
-        }
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-          if (!changed[m]) continue;
-          const int live = min(kPage, len - (i0 + m) * kPage);
-          const u32x4 x = base[m] ? reduce<F8 ? kNibbles : kBytes>(w[m], live, lane) : reduce<F8 ? kBytes : kWords>(w[m], live, lane);
-          if (lane < 32) {
-            char* dst = static_cast<char*>(a.bounds) +
-                        (((size_t)s * hkv + kvh) * b.max_blocks + (i0 + m)) * (2 * kHeadDim * kElem) + lane * 8 * kElem;
-            if constexpr (F8)
-              *reinterpret_cast<u32x2*>(dst) = u32x2{perm(x[1], x[0], 0x07050301u), perm(x[3], x[2], 0x07050301u)};   // the high bytes
-            else
-              *reinterpret_cast<u32x4*>(dst) = x;
-          }
-        }
-        if (++u == end) return;
+  int base_lo, base_hi;
+  bool by_tags;
+  auto enter = [&]() {
+    len = uniform(__builtin_amdgcn_readlane(len_lane, s - window));
+    from = uniform(__builtin_amdgcn_readlane(from_lane, s - window));
+    base_lo = base_hi = 0;
+    by_tags = ELASTIC && b.tags;
+    if (ELASTIC && b.base) {
+      const int p0 = b.base[2 * s], p1 = b.base[2 * s + 1];
+      if (p0 >= 0) {
+        by_tags = false;
+        base_lo = 2 * p0;
+        base_hi = 2 * p1;
       }
     }
-    kvh = j = 0;
-    do {   // the next sequence with a changed block (one exists: u < end)
+  };
+  // Lane l: physical block l of the 32 pairs from pair `entries` on, with its tag in the sign.
+  int entries = 0, entry_lane = 0;
+  auto read_entries = [&]() {
+    entries = j;
+    const int i = 2 * (from / 2 + j) + lane;
+    entry_lane = 0;
+    if (i * kPage < len) {
+      const size_t at = (size_t)s * b.max_blocks + i;
+      const int entry = b.bt[at];
+      const uint8_t tag = (by_tags ? b.tags : reinterpret_cast<const uint8_t*>(b.bt))[at];   // (one round trip)
+      entry_lane = (unsigned)entry < (unsigned)b.num_blocks ? entry : 0;   // never leave the pool
+      if (ELASTIC && by_tags && tag != 0) entry_lane |= 1 << 31;
+    }
+  };
+  enter();
+  read_entries();
+
+  // A unit on its way: where its bounds go, and of each block the tokens that count (0: not changed) and the mode.
+  struct Unit {
+    Row w[2][4];
+    size_t to;
+    int live[2];
+    bool base[2];
+  };
+  // of the current pair of the sequence, as entered at its first head
+  const char* tile[2];
+  int live[2];
+  bool base[2];
+  uint32_t off[2], step[2];
+  const uint32_t target_row = kHeadDim * kElem, base_row = target_row / 2;
+  const uint32_t target_off = (lane >> 4) * target_row + (lane & 15) * (target_row / 16),
+                 base_off = (lane >> 4) * base_row + (lane & 14) * (base_row / 16);
+  auto enter_pair = [&]() {
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const int i = uniform(2 * (from / 2 + j) + m), at = uniform(2 * (j - entries) + m);
+      const bool changed = i >= uniform(from) && i * kPage < uniform(len);   // (one of the two is; the other's loads go to any block)
+      const int entry = __builtin_amdgcn_readlane(entry_lane, at);
+      live[m] = changed ? min(kPage, uniform(len) - i * kPage) : 0;
+      base[m] = ELASTIC && changed && (by_tags ? entry < 0 : (i >= base_lo && i < base_hi));
+      tile[m] = reinterpret_cast<const char*>(b.pool) + (size_t)(entry & 0x7FFFFFFF) * 2 * hkv * kTile + (base[m] ? m * (kTile / 2) : 0);
+      off[m] = base[m] ? base_off : target_off;
+      step[m] = base[m] ? 4 * base_row : 4 * target_row;
+    }
+  };
+  enter_pair();
+  auto load = [&](Unit& u) {   // the unit at (s, j, kvh); then moves on
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const char* src = tile[m] + (size_t)kvh * kTile;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        uint32_t at = off[m] + r * step[m];
+        asm volatile("" : "+v"(at));   // (opaque: the load then takes a scalar base and this offset)
+        u.w[m][r] = __builtin_nontemporal_load(reinterpret_cast<const Row*>(src + at));
+      }
+      u.live[m] = live[m];
+      u.base[m] = base[m];
+    }
+    u.to = (((size_t)s * hkv + kvh) * b.max_blocks + 2 * (from / 2 + j)) * (2 * kHeadDim * kElem);
+  };
+  auto advance = [&]() {
+    if (++kvh < hkv) return;
+    kvh = 0;
+    j = uniform(j + 1);
+    if (j == uniform(np)) {
+      j = 0;
+      uint64_t hit;
+      int x;
       ++s;
-      np = pairs(s);
-    } while (np == 0);
+      while (true) {   // the next sequence with a changed block (one exists while units are left)
+        if (s - window >= 64) read_lengths(s);
+        x = pairs_lane();
+        hit = __builtin_amdgcn_ballot_w64(x > 0 && lane >= s - window);
+        if (hit) break;
+        s = window + 64;
+      }
+      s = uniform(window + __builtin_ctzll(hit));
+      np = __builtin_amdgcn_readlane(x, s - window);
+      enter();
+      read_entries();
+    } else if (uniform(j - entries) == 32) {
+      read_entries();
+    }
+    enter_pair();
+  };
+  auto finish = [&](const Unit& u) {   // (blocks that are not changed are reduced too: what was loaded has to be waited for)
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      uint32_t low, high;
+      if (ELASTIC && u.base[m]) reduce<F8 ? kNibbles : kBytes, F8>(u.w[m], u.live[m], lane, low, high);
+      else reduce<F8 ? kBytes : kWords, F8>(u.w[m], u.live[m], lane, low, high);
+      if (u.live[m] > 0) {
+        char* dst = static_cast<char*>(a.bounds) + u.to + m * (2 * kHeadDim * kElem) + (8 * (lane & 15) + 2 * (lane >> 4)) * kElem;
+        if constexpr (F8) {   // the high bytes
+          *reinterpret_cast<uint16_t*>(dst) = (uint16_t)perm(0u, low, 0x0C0C0301u);
+          *reinterpret_cast<uint16_t*>(dst + kHeadDim) = (uint16_t)perm(0u, high, 0x0C0C0301u);
+        } else {
+          *reinterpret_cast<uint32_t*>(dst) = low;
+          *reinterpret_cast<uint32_t*>(dst + 2 * kHeadDim) = high;
+        }
+      }
+    }
+  };
+  Unit one, two;
+  load(one);
+#pragma unroll 1
+  for (uint32_t u = begin;; u += 2) {   // (the last unit is loaded again rather than none: the loads stay countable)
+    if (u + 1 < end) advance();
+    load(two);
+    finish(one);
+    if (u + 1 >= end) return;
+    if (u + 2 < end) advance();
+    load(one);
+    finish(two);
+    if (u + 2 >= end) return;
   }
 }
 
@@ -258,10 +345,12 @@ __global__ __launch_bounds__(64 * kWaves) void key_bounds_kernel(BoundsArgs a) {
 
 hipError_t launch_key_bounds(const BoundsArgs& a, int dtype, bool elastic, hipStream_t st) {
   if (a.rows.batch == 0) return hipSuccess;
-  // at most the pairs there can be, and 32 waves a compute unit
-  const int64_t most = (int64_t)a.rows.batch * a.rows.num_kv_heads * ((a.rows.len_cap + 2 * kPage - 1) / (2 * kPage));
-  const dim3 grid((unsigned)std::max<int64_t>(1, std::min<int64_t>((most + kWaves - 1) / kWaves, 2048))), block(64 * kWaves);
+  // As many workgroups as there can be pairs of blocks, at most two waves a SIMD, of 8-bit pools, whose units are half as
+  // many bytes, four: 164 thousand 16-bit tokens of 8 heads 81.5 us (four waves: 84.0, eight, in turn: 88.1), 600 thousand
+  // 8-bit ones, half of them BASE, 117 (two waves: 125).
   const bool f8 = dtype == 3;
+  const int64_t most = (int64_t)a.rows.batch * a.rows.num_kv_heads * ((a.rows.len_cap + 2 * kPage - 1) / (2 * kPage));
+  const dim3 grid((unsigned)std::max<int64_t>(1, std::min<int64_t>((most + kWaves - 1) / kWaves, f8 ? 1024 : 512))), block(64 * kWaves);
   if (f8 && elastic) hipLaunchKernelGGL((key_bounds_kernel<true, true>), grid, block, 0, st, a);
   else if (f8) hipLaunchKernelGGL((key_bounds_kernel<true, false>), grid, block, 0, st, a);
   else if (elastic) hipLaunchKernelGGL((key_bounds_kernel<false, true>), grid, block, 0, st, a);

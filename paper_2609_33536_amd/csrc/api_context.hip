@@ -54,10 +54,32 @@ ekv_status check_budget(int32_t budget) {
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Scratch of a selection: [keys u64, a row per (sequence, KV head)]
-size_t select_bytes(const ekv_pool* pool, const ekv_batch* b, int32_t budget) {
-  const int blocks = max_seq_blocks(b);
-  return blocks <= budget || b->batch == 0 ? 256 : align256((size_t)b->batch * pool->num_kv_heads * blocks * sizeof(uint64_t));
+// Scratch of a selection whose rows take several chunks: [keys u64 | block numbers], 256-B aligned parts.
+// (The chunks keep the most with no first and newest blocks.)
+struct SelectLayout {
+  size_t blocks, total;
+};
+SelectLayout select_layout(const SelectArgs& a) {
+  const size_t kept = a.chunks > 1 ? (size_t)a.batch * a.num_kv_heads * a.chunks * a.kept : 0;
+  SelectLayout l{};
+  l.blocks = align256(kept * sizeof(uint64_t));
+  l.total = std::max<size_t>(256, l.blocks + align256(kept * sizeof(int32_t)));
+  return l;
+}
+SelectArgs select_args(const ekv_pool* pool, const ekv_batch* b, int group, int32_t budget, int32_t sink, int32_t recent) {
+  const BlockRows rows = block_rows(pool, b);
+  SelectArgs a{};
+  a.lens = rows.lens;
+  a.batch = rows.batch;
+  a.num_kv_heads = rows.num_kv_heads;
+  a.group = group;
+  a.max_blocks = rows.max_blocks;
+  a.len_cap = rows.len_cap;
+  a.budget = budget;
+  a.sink = sink;
+  a.recent = recent;
+  plan_select(&a, max_seq_blocks(b));
+  return a;
 }
 
 // Scratch of a decode over selected blocks: [merge counters | (m, l) | o], 256-B aligned parts
@@ -106,8 +128,8 @@ ekv_status ekv_key_bounds(const ekv_pool* pool, const ekv_batch* batch, const in
     int group = 0;
     ekv_status st = check_rows(pool, batch, &group);
     if (st != EKV_OK) return st;
-    if ((int64_t)batch->batch * (max_seq_blocks(batch) + 1) / 2 >= (1LL << 31))
-      return fail(EKV_ERR_UNSUPPORTED, "ekv_key_bounds: the batch must have fewer than 2^32 blocks");
+    if ((int64_t)batch->batch * pool->num_kv_heads * ((max_seq_blocks(batch) + 1) / 2) >= (1LL << 31))
+      return fail(EKV_ERR_UNSUPPORTED, "ekv_key_bounds: the batch has too many blocks for one call");
     if (batch->batch == 0) return EKV_OK;
     if (!bounds) return fail(EKV_ERR_INVALID, "bounds is NULL");
     if (!aligned16(bounds) || !aligned16(pool->kv)) return fail(EKV_ERR_INVALID, "bounds and the pool must be 16-byte aligned");
@@ -123,7 +145,7 @@ ekv_status ekv_key_bounds(const ekv_pool* pool, const ekv_batch* batch, const in
 size_t ekv_select_workspace_bytes(const ekv_pool* pool, const ekv_batch* batch, int32_t budget) {
   int group = 0;
   if (check_rows(pool, batch, &group) != EKV_OK || check_budget(budget) != EKV_OK) return 0;
-  return select_bytes(pool, batch, budget);
+  return select_layout(select_args(pool, batch, group, budget, 0, 0)).total;
 }
 
 ekv_status ekv_select_blocks(const ekv_pool* pool, const ekv_batch* batch, const void* q, const void* bounds, int32_t budget,
@@ -136,33 +158,24 @@ ekv_status ekv_select_blocks(const ekv_pool* pool, const ekv_batch* batch, const
     if ((st = check_budget(budget)) != EKV_OK) return st;
     if (sink < 0 || recent < 0 || (int64_t)sink + recent > budget)
       return fail(EKV_ERR_INVALID, "sink and recent must not be negative, nor their sum exceed the budget");
-    if ((int64_t)batch->batch * pool->num_kv_heads * ((max_seq_blocks(batch) + 255) / 256) > kMostRows)
+    if ((int64_t)batch->batch * pool->num_kv_heads * ((max_seq_blocks(batch) + 511) / 512) > kMostRows)
       return fail(EKV_ERR_UNSUPPORTED, "ekv_select_blocks: the batch has too many blocks for one call");
     if (batch->batch == 0) return EKV_OK;
     if (!q || !bounds || !selected || !counts) return fail(EKV_ERR_INVALID, "q, bounds, selected and counts are required");
-    const size_t need = select_bytes(pool, batch, budget);
+    SelectArgs a = select_args(pool, batch, group, budget, sink, recent);
+    const SelectLayout l = select_layout(a);
+    const size_t need = l.total;
     if (!ws || ws_bytes < need)
       return fail(EKV_ERR_INVALID, "workspace of %zu bytes needed, %zu given", need, ws ? ws_bytes : (size_t)0);
     if (!aligned16(q) || !aligned16(bounds) || !aligned16(ws))
       return fail(EKV_ERR_INVALID, "q, bounds and ws must be 16-byte aligned");
     if (debug_mode() && (st = debug_check_batch(pool, batch, stream, "ekv_select_blocks")) != EKV_OK) return st;
-    const BlockRows rows = block_rows(pool, batch);
-    SelectArgs a{};
-    a.lens = rows.lens;
     a.q = static_cast<const uint16_t*>(q);
     a.bounds = bounds;
     a.selected = selected;
     a.counts = counts;
     a.keys = static_cast<uint64_t*>(ws);
-    a.batch = rows.batch;
-    a.num_kv_heads = rows.num_kv_heads;
-    a.group = group;
-    a.max_blocks = rows.max_blocks;
-    a.len_cap = rows.len_cap;
-    a.budget = budget;
-    a.sink = sink;
-    a.recent = recent;
-    a.key_stride = max_seq_blocks(batch);
+    a.blocks = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + l.blocks);
     return hip_status(launch_select(a, pool->dtype, stream), "ekv_select_blocks launch");
   });
 }

@@ -32,11 +32,16 @@ struct SelectArgs {
   const void* bounds;        // as above
   int32_t* selected;         // [B][Hkv][budget]
   int32_t* counts;           // [B][Hkv]
-  uint64_t* keys;            // [B Hkv][key_stride] scratch
   int32_t batch, num_kv_heads, group, max_blocks, len_cap;
   int32_t budget, sink, recent;
-  int32_t key_stride;        // blocks of the longest sequence
+  // A row is scored in chunks; with more than one, each keeps its `kept` best, as
+  // scores' keys and block numbers (set by plan_select):
+  int32_t chunk, chunks, kept;
+  uint64_t* keys;            // [B Hkv][chunks][kept] scratch
+  int32_t* blocks;           // the same shape
 };
+// Fills in the chunks for rows of at most `blocks` blocks.
+void plan_select(SelectArgs* a, int blocks);
 hipError_t launch_select(const SelectArgs& a, int dtype, hipStream_t st);
 
 struct SelectedArgs {

@@ -6,12 +6,15 @@
 // heads.  Scores are summed in 64 bits: products of 16-bit values are exact there and so are, as a rule, their
 // sums, so that the order of near neighbours does not depend on the order of the sum.
 //
-// score_kernel: a wave takes 64 blocks, a lane 8 channels (16 of 8-bit bounds) of one bound,
-// fixed for all of its loads, so that its share of the query stays in registers.  The partial sums
-// of 32 (16) loads are summed over the lanes and dealt out to them in one go, half of them a step,
-// and lane l ends up with the score of block l.  It is bound by HBM: 512 bytes of bounds a block.
-// select_kernel: one workgroup a row finds the budget's last score by histograms of what is still
-// in question, and lists the blocks above it in order.
+// A wave takes 16 blocks (32 of 8-bit bounds) at a time in 8 loads, a lane 8 (16) channels of one
+// bound, fixed for all of its loads, so that its share of the query stays in registers.  The partial
+// sums of the 8 loads are summed over the lanes and dealt out to them in one go, half of them a
+// step.  This is bound by HBM: 512 (256) bytes of bounds a block.
+//
+// scan_kernel: a workgroup scores a chunk of a row's blocks into LDS, finds the budget's last score
+// by histograms of what is still in question, and lists the blocks above it in order.  Where a
+// row is one chunk, that is the result.  Else the chunk's own best, as many as the budget could
+// take of it, go to the workspace, and join_kernel picks among those of all chunks the same way.
 #include <algorithm>
 
 #include "common.h"
@@ -21,10 +24,8 @@
 namespace ekv {
 namespace {
 
-constexpr int kTileBlocks = 64;
-
-// A score as an integer that orders as it does: 0 below all scores, kForced above them, what is not a number next to that.
-constexpr uint64_t kForced = ~0ull, kNotNumber = ~1ull;
+// A score as an integer that orders as it does, above 1; what is not a number above all scores.
+constexpr uint64_t kNotNumber = ~0ull;
 __device__ __forceinline__ uint64_t score_key(double x) {
   if (x != x) return kNotNumber;
   const uint64_t w = __builtin_bit_cast(uint64_t, x + 0.0);   // (-0 is 0)
@@ -82,68 +83,91 @@ __device__ __forceinline__ double dot(u32x4 w, const double (&q)[C]) {
   return s;
 }
 
-// The sums of loads u, u + 2^B, .. (all that share the bits below B with u), dealt out to lane bits B and up.
-// w holds a batch's loads in the order of their bits from B0 on.
-template <typename T, bool F8, int TOP, int B0, int B, int U, int C>
+// The sums of the loads U, U + 2^(B - B0), .. of w, dealt out to lane bits B0 (the last bit of a load's number) to TOP.
+template <typename T, bool F8, int TOP, int B, int U, int C>
 __device__ __forceinline__ double node(const u32x4* w, const double (&q)[C], int lane) {
-  if constexpr (B == TOP) return dot<T, F8>(w[U], q);
+  if constexpr (B > TOP) return dot<T, F8>(w[U], q);
   else {
-    const double a = node<T, F8, TOP, B0, B + 1, U>(w, q, lane);
-    const double b = node<T, F8, TOP, B0, B + 1, (U | 1 << (B - B0))>(w, q, lane);
+    const double a = node<T, F8, TOP, B + 1, U>(w, q, lane);
+    const double b = node<T, F8, TOP, B + 1, (U | 1 << (B - TOP + 2))>(w, q, lane);
     return halved<B>(a, b, lane);
   }
 }
 
-// Scores of blocks t0 .. t0 + 63 of a row of bounds, one a lane (blocks from n on: of no meaning).
+// The sums over a KV head's query heads of what is above and below zero, for each channel: [below | above].
+struct Query {
+  double part[4][2 * kHeadDim];
+};
+// queries [group][128] of the KV head.  Every thread of the workgroup; ends with a barrier.  meanwhile() is called with the
+// loads on their way.
+template <typename T, typename F>
+__device__ __forceinline__ void sum_queries(const uint16_t* src, int group, Query& sm, F meanwhile) {
+  const int c = threadIdx.x % kHeadDim, share = threadIdx.x / kHeadDim;   // heads share, share + 4, ..
+  uint16_t w[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) w[k] = src[min(share + 4 * k, group - 1) * kHeadDim + c];
+  __builtin_amdgcn_sched_barrier(0);   // (in this order: what is loaded meanwhile is not waited for)
+  meanwhile();
+  double below = 0.0, above = 0.0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float x = share + 4 * k < group ? Mma<T>::widen(w[k]) : 0.f;
+    below += (double)(x < 0.f ? x : 0.f);   // (a NaN counts as nothing)
+    above += (double)(x > 0.f ? x : 0.f);
+  }
+  sm.part[share][c] = below;
+  sm.part[share][kHeadDim + c] = above;
+  __syncthreads();
+}
+
+// Scores of the blocks of a row of bounds.
 template <typename T, bool F8>
 struct Scorer {
-  static constexpr int kLoads = F8 ? 16 : 32, kTop = F8 ? 4 : 5, kChannels = F8 ? 16 : 8;
-  static constexpr int kRowBytes = F8 ? 2 * kHeadDim : 4 * kHeadDim;   // of one block
+  static constexpr int kSpan = F8 ? 16 : 32, kTop = F8 ? 3 : 4, kChannels = F8 ? 16 : 8;   // lanes of a block; their number's last bit
+  static constexpr int kTile = 8 * 64 / kSpan;                                             // blocks of 8 loads
+  static constexpr int kRowBytes = F8 ? 2 * kHeadDim : 4 * kHeadDim;                       // of one block
+  const char* row;     // block 0
+  int lane, n;
   double q[kChannels];
-  int lane;
+  u32x4 w[2][8];
 
-  // queries [group][128] of the KV head
-  __device__ __forceinline__ void queries(const uint16_t* src, int group) {
-    const int c0 = kChannels * (lane % (kLoads / 2));
-    const bool high = lane % kLoads >= kLoads / 2;   // the lane holds upper bounds
+  __device__ __forceinline__ void load(u32x4 (&to)[8], int t) const {   // a tile (blocks from n on: the last again)
+    const uint32_t at = (lane % kSpan) * 16;
 #pragma unroll
-    for (int i = 0; i < kChannels; ++i) q[i] = 0.0;
-#pragma unroll 1
-    for (int g = 0; g < group; ++g) {
-#pragma unroll
-      for (int h = 0; h < kChannels / 8; ++h) {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(src + g * kHeadDim + c0 + 8 * h);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float x = Mma<T>::widen((uint16_t)(w[i >> 1] >> (16 * (i & 1))));
-          q[8 * h + i] += (double)(high ? (x > 0.f ? x : 0.f) : (x < 0.f ? x : 0.f));
-        }
-      }
+    for (int u = 0; u < 8; ++u) {
+      const uint32_t block = min(t + lane / kSpan * 8 + u, n - 1);
+      to[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(row + (block * kRowBytes + at)));
     }
+    asm volatile("" ::: "memory");   // (else each load is moved to its use)
+    __builtin_amdgcn_sched_barrier(0);
   }
+  __device__ __forceinline__ void queries(const Query& sm) {
+    const int c0 = (lane % kSpan >= kSpan / 2 ? kHeadDim : 0) + kChannels * (lane % (kSpan / 2));   // (lower or upper bounds)
+#pragma unroll
+    for (int i = 0; i < kChannels; ++i) q[i] = (sm.part[0][c0 + i] + sm.part[1][c0 + i]) + (sm.part[2][c0 + i] + sm.part[3][c0 + i]);
+  }
+  // The score of block `of(t)` of the tile.
+  __device__ __forceinline__ double sum(const u32x4 (&from)[8]) const {
+    double x = node<T, F8, kTop, kTop - 2, 0>(from, q, lane);
+    if constexpr (!F8) x += moved<0x4E>(x);   // (lanes l ^ 2)
+    return x + moved<0xB1>(x);                // (lanes l ^ 1)
+  }
+  __device__ __forceinline__ int of(int t) const { return t + lane / kSpan * 8 + (lane >> (kTop - 2)) % 8; }
 
-  __device__ __forceinline__ double score(const char* row, int t0, int n) const {
-    // 8 loads (bits 2 and up of their number) at a time, 2 batches in flight
-    constexpr int kBatches = kLoads / 8, kB0 = kTop - 3;
-    const uint32_t at = (lane % kLoads) * 16;
-    const int mine = t0 + (lane / kLoads) * kLoads;
-    auto load = [&](u32x4 (&w)[8], int batch) {
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const int block = min(mine + batch + u * kBatches, n - 1);
-        w[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(row + (size_t)block * kRowBytes + at));
-      }
-    };
-    u32x4 w[2][8];
-    double part[kBatches];
-    load(w[0], 0);
-#pragma unroll
-    for (int k = 0; k < kBatches; ++k) {
-      if (k + 1 < kBatches) load(w[(k + 1) & 1], k + 1);
-      part[k] = node<T, F8, kTop, kB0, kB0, 0>(w[k & 1], q, lane);
+  // put(i, score of block i) for the blocks of tiles first, first + stride, .. below n, each by one lane; tile `first` is
+  // loaded already.  A tile's loads are in flight while the one before it is summed.
+  template <typename F>
+  __device__ __forceinline__ void scores(int first, int stride, F put) {
+    const bool mine = lane % (1 << (kTop - 2)) == 0;
+#pragma unroll 1
+    for (int t = first; t < n; t += 2 * stride) {
+      load(w[1], t + stride);
+      const double a = sum(w[0]);
+      if (mine && of(t) < n) put(of(t), a);
+      load(w[0], t + 2 * stride);
+      const double b = sum(w[1]);
+      if (mine && of(t + stride) < n) put(of(t + stride), b);
     }
-    if constexpr (F8) return halved<0>(part[0], part[1], lane);
-    else return halved<0>(halved<1>(part[0], part[2], lane), halved<1>(part[1], part[3], lane), lane);
   }
 };
 
@@ -151,218 +175,365 @@ __device__ __forceinline__ int blocks_of(const SelectArgs& a, int s) {
   return (min(max(a.lens[s], 0), a.len_cap) + kPage - 1) / kPage;
 }
 
-constexpr int kScoreWaves = 4;
-
-// Workgroup (row, part): 4 waves, 64 blocks each.  Rows that fit the budget need no scores.
-template <typename T, bool F8>
-__global__ __launch_bounds__(64 * kScoreWaves) void score_kernel(SelectArgs a, int parts) {
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int row = blockIdx.x / (unsigned)parts, part = blockIdx.x - row * parts, s = row / (unsigned)a.num_kv_heads;
-  const int n = blocks_of(a, s), t0 = (part * kScoreWaves + wave) * kTileBlocks;
-  if (n <= a.budget || t0 >= n) return;
-  Scorer<T, F8> sc;
-  sc.lane = lane;
-  sc.queries(a.q + (size_t)row * a.group * kHeadDim, a.group);
-  const char* bounds = static_cast<const char*>(a.bounds) + (size_t)row * a.max_blocks * Scorer<T, F8>::kRowBytes;
-  const double x = sc.score(bounds, t0, n);
-  const int i = t0 + lane;
-  if (i < n) a.keys[(size_t)row * a.key_stride + i] = i < a.sink || i >= n - a.recent ? kForced : score_key(x);
-}
-
-constexpr int kSelectWaves = 8, kBins = 1024;
-
-struct SelectShared {
-  uint32_t bins[kBins];
-  uint64_t low[kSelectWaves], high[kSelectWaves];
-  uint64_t list[64];
-  int above[kSelectWaves], equal[kSelectWaves];
-  int listed, bin, over;      // the list's length; the bin in question and how many lie above it
-  uint64_t last;              // the last score that is taken, and how many equal to it are
-  int ties;
-};
+constexpr int kBins = 1024, kRanked = 64;
 
 // (of one type: mixed 64-bit types would be compared as doubles)
 __device__ __forceinline__ uint64_t lower(uint64_t a, uint64_t b) { return a < b ? a : b; }
 __device__ __forceinline__ uint64_t higher(uint64_t a, uint64_t b) { return a < b ? b : a; }
 
-__device__ __forceinline__ uint64_t wave_min(uint64_t x) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) x = lower(x, __shfl_xor((unsigned long long)x, d));
-  return x;
-}
-__device__ __forceinline__ uint64_t wave_max(uint64_t x) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) x = higher(x, __shfl_xor((unsigned long long)x, d));
-  return x;
-}
-
-// Finds sm.last and sm.ties such that the keys of [lo, hi) above `last` and the first `ties` equal to it are
-// `need` in all (0 < need < hi - lo).  Every thread of the workgroup.
-__device__ void find_last(const uint64_t* keys, int lo, int hi, int need, SelectShared& sm) {
-  constexpr int kThreads = 64 * kSelectWaves;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// Smallest and largest key seen; key 0 is none.
+struct Range {
   uint64_t from = ~0ull, to = 0;
-  for (int i = lo + threadIdx.x; i < hi; i += kThreads) {
-    const uint64_t k = keys[i];
-    from = lower(from, k);
+  __device__ __forceinline__ void add(uint64_t k) {
+    if (k != 0) from = lower(from, k);
     to = higher(to, k);
   }
-  from = wave_min(from);
-  to = wave_max(to);
-  if (lane == 0) {
-    sm.low[wave] = from;
-    sm.high[wave] = to;
+  template <int CTRL>
+  __device__ __forceinline__ void step() {
+    from = lower(from, __builtin_bit_cast(uint64_t, moved<CTRL>(__builtin_bit_cast(double, from))));
+    to = higher(to, __builtin_bit_cast(uint64_t, moved<CTRL>(__builtin_bit_cast(double, to))));
   }
-  __syncthreads();
-  from = sm.low[0];
-  to = sm.high[0];
+  __device__ __forceinline__ void over_row() {   // of 16 lanes
+    step<0xB1>();    // quad_perm 1,0,3,2
+    step<0x4E>();    // quad_perm 2,3,0,1
+    step<0x141>();   // row_half_mirror
+    step<0x140>();   // row_mirror
+  }
+};
+
+// A pick among up to 2^31 keys by WAVES waves, AHEAD loads of keys in flight.
+template <int WAVES, int AHEAD>
+struct Picker {
+  static constexpr int kThreads = 64 * WAVES;
+  struct Shared {
+    uint32_t bins[kBins];
+    uint64_t low[4 * WAVES], high[4 * WAVES];
+    uint64_t list[kRanked];
+    int above[WAVES], equal[WAVES];
+    int listed, bin, over;      // the list's length; the bin in question and how many lie above it
+    uint64_t last;              // the last key that is taken, and how many equal to it are
+    int ties;
+  };
+
+  static __device__ __forceinline__ uint64_t lane_key(uint64_t x, int l) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), l) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, l);
+  }
+
+  // f(key) for this thread's share of keys [lo, hi).
+  template <typename F>
+  static __device__ __forceinline__ void each_key(const uint64_t* keys, int lo, int hi, F f) {
+    int i = lo + (int)threadIdx.x;
+    if constexpr (AHEAD > 1) {
+#pragma unroll 1
+      for (; i + (AHEAD - 1) * kThreads < hi; i += AHEAD * kThreads) {
+        uint64_t k[AHEAD];
 #pragma unroll
-  for (int w = 1; w < kSelectWaves; ++w) {
-    from = lower(from, sm.low[w]);
-    to = higher(to, sm.high[w]);
-  }
-  while (true) {   // the last key lies in [from, to], `need` of those from the top; each pass divides the range by 512 or more
-    if (from == to) {
-      if (threadIdx.x == 0) {
-        sm.last = from;
-        sm.ties = need;
+        for (int u = 0; u < AHEAD; ++u) k[u] = keys[i + u * kThreads];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) f(k[u]);
       }
-      break;
     }
-    const int shift = max(0, 54 - __builtin_clzll(to - from));   // (to - from) >> shift < 1024
+#pragma unroll 1
+    for (; i < hi; i += kThreads) f(keys[i]);
+  }
+
+  // Lane l's key of count <= 64 (0: none) ranked among them: sm.last and sm.ties for the largest `need`.
+  static __device__ __forceinline__ void rank(uint64_t k, int count, int need, Shared& sm) {
+    int above = 0, equal = 0;
+    for (int j0 = 0; j0 < count; j0 += 4) {   // (lanes from count on hold 0, which is above nothing)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint64_t o = lane_key(k, j0 + j);
+        above += o > k;
+        equal += o == k;
+      }
+    }
+    if (k != 0 && above < need && above + equal >= need) {   // (equal keys write the same)
+      sm.last = k;
+      sm.ties = need - above;
+    }
+  }
+
+  // Finds sm.last and sm.ties such that the keys of [lo, hi) above `last` and the first `ties` equal to it are
+  // `need` in all (0 < need < the number of keys there).  Every thread of the workgroup, each with the range of the keys
+  // that it has seen; the keys are as written before the call.
+  static __device__ __forceinline__ void find_last(const uint64_t* keys, int lo, int hi, int need, Range seen, Shared& sm) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (hi - lo <= kRanked) {
+      __syncthreads();
+      if (wave == 0) rank(lo + lane < hi ? keys[lo + lane] : 0, hi - lo, need, sm);
+      __syncthreads();
+      return;
+    }
+    seen.over_row();
+    if (lane % 16 == 0) {
+      sm.low[threadIdx.x / 16] = seen.from;
+      sm.high[threadIdx.x / 16] = seen.to;
+    }
     for (int i = threadIdx.x; i < kBins; i += kThreads) sm.bins[i] = 0;
     if (threadIdx.x == 0) sm.listed = 0;
     __syncthreads();
-    for (int i = lo + threadIdx.x; i < hi; i += kThreads) {
-      const uint64_t k = keys[i];
-      if (k >= from && k <= to) atomicAdd(&sm.bins[(k - from) >> shift], 1u);
-    }
-    __syncthreads();
-    if (wave == 0) {   // bins from the top, 16 a lane: the one in which the count reaches `need`
-      int mine = 0;
+    Range all;   // (each row of 16 lanes: 16 of the 4 * WAVES ranges)
+    all.from = sm.low[lane % (4 * WAVES)];
+    all.to = sm.high[lane % (4 * WAVES)];
+    all.over_row();
+    uint64_t from = ~0ull, to = 0;
 #pragma unroll
-      for (int b = 0; b < kBins / 64; ++b) mine += sm.bins[kBins - 1 - (lane * (kBins / 64) + b)];
-      const int incl = sum_scan(mine);
-      const uint64_t hit = __builtin_amdgcn_ballot_w64(incl >= need);
-      if (lane == (hit ? __builtin_ctzll(hit) : 63)) {
-        int over = incl - mine, b = kBins - 1 - lane * (kBins / 64);
-        while (b > 0 && over + (int)sm.bins[b] < need) over += sm.bins[b--];
-        sm.bin = b;
-        sm.over = over;
-      }
+    for (int r = 0; r < WAVES / 4; ++r) {
+      from = lower(from, lane_key(all.from, 16 * r));
+      to = higher(to, lane_key(all.to, 16 * r));
     }
-    __syncthreads();
-    const uint64_t bottom = from + ((uint64_t)sm.bin << shift);
-    const int count = sm.bins[sm.bin];
-    need -= sm.over;
-    from = bottom;
-    to = lower(to, bottom + ((1ull << shift) - 1));
-    if (need == count) {   // all of the bin (keys are never 0: nothing equals `bottom - 1` that is not below the bin)
-      if (threadIdx.x == 0) {
-        sm.last = bottom - 1;
-        sm.ties = 0;
-      }
-      break;
-    }
-    if (count <= 64 && from != to) {   // few: ranked among themselves
-      for (int i = lo + threadIdx.x; i < hi; i += kThreads) {
-        const uint64_t k = keys[i];
-        if (k >= from && k <= to) sm.list[atomicAdd(&sm.listed, 1) & 63] = k;
+    while (from < to) {   // the last key lies in [from, to], `need` of those from the top; a pass divides the range by 512 or more
+      const int shift = max(0, 54 - __builtin_clzll(to - from));   // (to - from) >> shift < 1024
+      each_key(keys, lo, hi, [&](uint64_t k) {
+        if (k >= from && k <= to) atomicAdd(&sm.bins[(k - from) >> shift], 1u);
+      });
+      __syncthreads();
+      if (wave == 0) {   // bins from the top, 16 a lane: the one in which the count reaches `need`
+        constexpr int kEach = kBins / 64;
+        int mine = 0;
+#pragma unroll
+        for (int b = 0; b < kEach; ++b) mine += sm.bins[kBins - 1 - (lane * kEach + b)];
+        const int incl = sum_scan(mine);
+        const uint64_t hit = __builtin_amdgcn_ballot_w64(incl >= need);
+        if (lane == (hit ? __builtin_ctzll(hit) : 63)) {
+          int over = incl - mine, b = kBins - 1 - lane * kEach;
+          while (b > 0 && over + (int)sm.bins[b] < need) over += sm.bins[b--];
+          sm.bin = b;
+          sm.over = over;
+        }
       }
       __syncthreads();
-      if (wave == 0) {
-        const uint64_t k = lane < count ? sm.list[lane] : 0;
-        int above = 0, equal = 0;
-        for (int j = 0; j < count; ++j) {
-          const uint64_t o = sm.list[j];
-          above += o > k;
-          equal += o == k;
-        }
-        if (lane < count && above < need && above + equal >= need) {   // (equal keys write the same)
-          sm.last = k;
-          sm.ties = need - above;
-        }
+      const int bin = __builtin_amdgcn_readfirstlane(sm.bin), count = __builtin_amdgcn_readfirstlane(sm.bins[bin]);
+      need -= __builtin_amdgcn_readfirstlane(sm.over);
+      from += (uint64_t)bin << shift;
+      to = lower(to, from + ((1ull << shift) - 1));
+      if (need == count) {   // all of the bin (no key is 0 or 1: none is taken for the one below it)
+        --from;
+        need = 0;
+        break;
       }
-      break;
+      if (count <= kRanked && from < to) {   // few: ranked among themselves
+        each_key(keys, lo, hi, [&](uint64_t k) {
+          if (k >= from && k <= to) sm.list[atomicAdd(&sm.listed, 1) % kRanked] = k;
+        });
+        __syncthreads();
+        if (wave == 0) rank(lane < count ? sm.list[lane] : 0, count, need, sm);
+        __syncthreads();
+        return;
+      }
+      __syncthreads();
+      for (int i = threadIdx.x; i < kBins; i += kThreads) sm.bins[i] = 0;
+      __syncthreads();
     }
-    __syncthreads();   // (the bins are cleared next)
+    if (threadIdx.x == 0) {
+      sm.last = from;
+      sm.ties = need;
+    }
+    __syncthreads();
   }
-  __syncthreads();
+
+  // put(place, i) for the keys i of [lo, hi) above `last` and the first `ties` equal to it, places 0, 1, .. in
+  // order.  Every thread of the workgroup.
+  template <typename F>
+  static __device__ __forceinline__ void list_above(const uint64_t* keys, int lo, int hi, uint64_t last, int ties, Shared& sm, F put) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // a wave's run of keys: how many it takes, then its places, then its keys in order
+    const int run = ((hi - lo + WAVES - 1) / WAVES + 63) / 64 * 64, begin = min(hi, lo + wave * run), end = min(hi, begin + run);
+    constexpr int kEach = AHEAD;
+    auto load = [&](int i0, uint64_t (&k)[kEach]) {
+#pragma unroll
+      for (int u = 0; u < kEach; ++u) k[u] = i0 + 64 * u + lane < end ? keys[i0 + 64 * u + lane] : 0;
+    };
+    int above = 0, equal = 0;
+#pragma unroll 1
+    for (int i0 = begin; i0 < end; i0 += 64 * kEach) {
+      uint64_t k[kEach];
+      load(i0, k);
+#pragma unroll
+      for (int u = 0; u < kEach; ++u) {
+        above += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k[u] > last));
+        equal += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k[u] == last));
+      }
+    }
+    if (lane == 0) {
+      sm.above[wave] = above;
+      sm.equal[wave] = equal;
+    }
+    __syncthreads();
+    int place = 0, seen = 0;   // keys taken, and keys equal to the last, before this wave's run
+    for (int w = 0; w < wave; ++w) {
+      place += sm.above[w] + min(sm.equal[w], max(0, ties - seen));
+      seen += sm.equal[w];
+    }
+    const uint64_t below = (1ull << lane) - 1;
+#pragma unroll 1
+    for (int i0 = begin; i0 < end; i0 += 64 * kEach) {
+      uint64_t k[kEach];
+      load(i0, k);
+#pragma unroll
+      for (int u = 0; u < kEach; ++u) {
+        const uint64_t eq = __builtin_amdgcn_ballot_w64(k[u] == last);
+        const bool take = k[u] > last || (k[u] == last && seen + __builtin_popcountll(eq & below) < ties);
+        const uint64_t all = __builtin_amdgcn_ballot_w64(take);
+        if (take) put(place + __builtin_popcountll(all & below), i0 + 64 * u + lane);
+        place += __builtin_popcountll(all);
+        seen += __builtin_popcountll(eq);
+      }
+    }
+  }
+};
+
+// A row's list but for the blocks picked by score: the first and newest blocks around them and -1 behind, or all
+// blocks if they fit the budget.  Returns whether a pick is to be made.
+template <int THREADS>
+__device__ __forceinline__ bool frame(const SelectArgs& a, int row, int n) {
+  int32_t* out = a.selected + (size_t)row * a.budget;
+  const bool all = n <= a.budget;
+  const int taken = all ? n : a.budget, first = all ? n : a.sink, newest = all ? 0 : a.recent;
+  if (threadIdx.x == 0) a.counts[row] = taken;
+  for (int i = threadIdx.x; i < first; i += THREADS) out[i] = i;
+  for (int i = threadIdx.x; i < newest; i += THREADS) out[taken - newest + i] = n - newest + i;
+  for (int i = taken + threadIdx.x; i < a.budget; i += THREADS) out[i] = -1;
+  return !all && a.sink + a.recent < a.budget;
 }
 
-__global__ __launch_bounds__(64 * kSelectWaves) void select_kernel(SelectArgs a) {
-  __shared__ SelectShared sm;
+constexpr int kScanWaves = 8;
+
+// Workgroup (row, chunk of a.chunk blocks)
+template <typename T, bool F8>
+__global__ __launch_bounds__(64 * kScanWaves, 4) void scan_kernel(SelectArgs a) {
+  typedef Picker<kScanWaves, 1> P;
+  extern __shared__ uint64_t keys[];   // [a.chunk]
+  __shared__ typename P::Shared sm;
+  __shared__ Query query;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int row = blockIdx.x, n = blocks_of(a, row / (unsigned)a.num_kv_heads), taken = min(n, a.budget);
-  int32_t* out = a.selected + (size_t)row * a.budget;
-  if (threadIdx.x == 0) a.counts[row] = taken;
-  for (int i = taken + threadIdx.x; i < a.budget; i += 64 * kSelectWaves) out[i] = -1;
-  if (n <= a.budget) {
-    for (int i = threadIdx.x; i < n; i += 64 * kSelectWaves) out[i] = i;
+  const int row = blockIdx.x / (unsigned)a.chunks, part = blockIdx.x - row * a.chunks, s = row / (unsigned)a.num_kv_heads;
+  const int n = blocks_of(a, s), c0 = part * a.chunk, need = a.budget - a.sink - a.recent;
+  if (a.chunks == 1) {
+    if (!frame<P::kThreads>(a, row, n)) return;
+  } else if (n <= a.budget || need == 0 || c0 >= n) {   // (the join sees to it)
     return;
   }
-  const uint64_t* keys = a.keys + (size_t)row * a.key_stride;
-  const int need = a.budget - a.sink - a.recent;
-  uint64_t last = kNotNumber;   // (none beyond the first and newest blocks)
+  const int c1 = min(n, c0 + a.chunk);
+  const int lo = max(a.sink, c0) - c0, hi = min(n - a.recent, c1) - c0;   // the chunk's blocks that are picked by score
+  Scorer<T, F8> sc;
+  sc.lane = lane;
+  sc.n = c1 - c0;   // (offsets in a chunk fit 32 bits)
+  sc.row = static_cast<const char*>(a.bounds) + ((size_t)row * a.max_blocks + c0) * Scorer<T, F8>::kRowBytes;
+  const int first = wave * Scorer<T, F8>::kTile;
+  static_assert(kScanWaves * 64 == 4 * kHeadDim, "a thread a channel and share of the heads");
+  sum_queries<T>(a.q + (size_t)row * a.group * kHeadDim, a.group, query, [&]() { sc.load(sc.w[0], first); });
+  Range seen;
+  if (first < sc.n) {
+    sc.queries(query);
+    sc.scores(first, kScanWaves * Scorer<T, F8>::kTile, [&](int i, double x) {
+      const uint64_t k = score_key(x);
+      keys[i] = k;
+      if (i >= lo && i < hi) seen.add(k);
+    });
+  }
+  uint64_t last = 0;   // (all)
   int ties = 0;
-  if (need > 0) {
-    find_last(keys, a.sink, n - a.recent, need, sm);
+  if (hi - lo > need) {
+    P::find_last(keys, lo, hi, need, seen, sm);
     last = sm.last;
     ties = sm.ties;
+  } else {
+    __syncthreads();
   }
-  // a wave's run of blocks: how many it takes, then its places, then its blocks in order
-  const int run = ((n + kSelectWaves - 1) / kSelectWaves + 63) / 64 * 64, begin = min(n, wave * run), end = min(n, begin + run);
-  int above = 0, equal = 0;
-  for (int i0 = begin; i0 < end; i0 += 64) {
-    const uint64_t k = i0 + lane < end ? keys[i0 + lane] : 0;
-    above += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k > last));
-    equal += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k == last));
-  }
-  if (lane == 0) {
-    sm.above[wave] = above;
-    sm.equal[wave] = equal;
-  }
-  __syncthreads();
-  int place = 0, seen = 0;   // blocks taken, and blocks equal to the last, before this wave's run
-  for (int w = 0; w < wave; ++w) {
-    place += sm.above[w] + min(sm.equal[w], max(0, ties - seen));
-    seen += sm.equal[w];
-  }
-  const uint64_t below = (1ull << lane) - 1;
-  for (int i0 = begin; i0 < end; i0 += 64) {
-    const uint64_t k = i0 + lane < end ? keys[i0 + lane] : 0;
-    const uint64_t eq = __builtin_amdgcn_ballot_w64(k == last);
-    const bool take = k > last || (k == last && seen + __builtin_popcountll(eq & below) < ties);
-    const uint64_t all = __builtin_amdgcn_ballot_w64(take);
-    const int at = place + __builtin_popcountll(all & below);
-    if (take && at < taken) out[at] = i0 + lane;   // (always, unless another call writes this workspace meanwhile)
-    place += __builtin_popcountll(all);
-    seen += __builtin_popcountll(eq);
+  if (a.chunks == 1) {
+    int32_t* out = a.selected + (size_t)row * a.budget + a.sink;
+    P::list_above(keys, lo, hi, last, ties, sm, [&](int place, int i) { out[place] = i; });
+  } else {
+    const size_t at = ((size_t)row * a.chunks + part) * a.kept;
+    P::list_above(keys, lo, max(lo, hi), last, ties, sm, [&](int place, int i) {
+      a.keys[at + place] = keys[i];
+      a.blocks[at + place] = c0 + i;
+    });
+    for (int i = max(0, min(need, hi - lo)) + threadIdx.x; i < a.kept; i += P::kThreads) a.keys[at + i] = 0;
   }
 }
 
+// Workgroup (row): picks among what the chunks kept, copied to LDS if it has room for it (LOCAL keys, or 0).
+template <int WAVES, int LOCAL>
+__global__ __launch_bounds__(64 * WAVES) void join_kernel(SelectArgs a) {
+  typedef Picker<WAVES, (LOCAL > 0 ? 2 : 8)> P;
+  __shared__ uint64_t local[LOCAL > 0 ? LOCAL : 1];
+  __shared__ int32_t local_blocks[LOCAL > 0 ? LOCAL : 1];
+  __shared__ typename P::Shared sm;
+  const int row = blockIdx.x, n = blocks_of(a, row / (unsigned)a.num_kv_heads);
+  if (!frame<P::kThreads>(a, row, n)) return;
+  const int kept = (n + a.chunk - 1) / a.chunk * a.kept, need = a.budget - a.sink - a.recent;
+  const size_t at = (size_t)row * a.chunks * a.kept;
+  const uint64_t* keys = a.keys + at;
+  const int32_t* blocks = a.blocks + at;
+  Range seen;
+  if constexpr (LOCAL > 0) {
+#pragma unroll 4
+    for (int i = threadIdx.x; i < kept; i += P::kThreads) {
+      const uint64_t k = keys[i];
+      local[i] = k;
+      local_blocks[i] = blocks[i];
+      seen.add(k);
+    }
+    keys = local;
+    blocks = local_blocks;
+  } else {
+    P::each_key(keys, 0, kept, [&](uint64_t k) { seen.add(k); });
+  }
+  uint64_t last = 0;
+  int ties = 0;
+  if (n - a.sink - a.recent > need) {
+    P::find_last(keys, 0, kept, need, seen, sm);
+    last = sm.last;
+    ties = sm.ties;
+  } else {
+    __syncthreads();
+  }
+  int32_t* out = a.selected + (size_t)row * a.budget + a.sink;
+  // (a place beyond `need` only if another call writes this workspace meanwhile)
+  P::list_above(keys, 0, kept, last, ties, sm, [&](int place, int i) {
+    if (place < need) out[place] = blocks[i];
+  });
+}
+
+constexpr int kFewKept = 4096, kManyKept = 12288;   // 48 and 144 KiB of LDS
+
 template <typename T, bool F8>
-void run_scores(const SelectArgs& a, hipStream_t st) {
-  const int parts = (a.key_stride + kScoreWaves * kTileBlocks - 1) / (kScoreWaves * kTileBlocks);
-  hipLaunchKernelGGL((score_kernel<T, F8>), dim3((unsigned)(a.batch * a.num_kv_heads * parts)), dim3(64 * kScoreWaves), 0, st, a, parts);
+hipError_t run_typed(const SelectArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL((scan_kernel<T, F8>), dim3((unsigned)(a.batch * a.num_kv_heads * a.chunks)), dim3(64 * kScanWaves),
+                     a.chunk * sizeof(uint64_t), st, a);
+  if (a.chunks > 1) {
+    const int64_t most = (int64_t)a.chunks * a.kept;
+    const dim3 grid((unsigned)(a.batch * a.num_kv_heads));
+    if (most <= kFewKept) hipLaunchKernelGGL((join_kernel<8, kFewKept>), grid, dim3(512), 0, st, a);
+    else if (most <= kManyKept) hipLaunchKernelGGL((join_kernel<16, kManyKept>), grid, dim3(1024), 0, st, a);
+    else hipLaunchKernelGGL((join_kernel<16, 0>), grid, dim3(1024), 0, st, a);
+  }
+  return hipGetLastError();
 }
 
 }  // namespace
 
+void plan_select(SelectArgs* a, int blocks) {
+  // Chunks of 512 to 4096 blocks (32 KiB of LDS), the largest that leave 240 workgroups of 8 waves
+  int chunk = 4096;
+  while (chunk > 512 && (int64_t)a->batch * a->num_kv_heads * ((blocks + chunk - 1) / chunk) < 240) chunk /= 2;
+  chunk = std::min(chunk, (blocks + 63) / 64 * 64);
+  a->chunk = std::max(chunk, 64);
+  a->chunks = std::max(1, (blocks + a->chunk - 1) / a->chunk);
+  a->kept = std::min(a->chunk, a->budget - a->sink - a->recent);
+}
+
 hipError_t launch_select(const SelectArgs& a, int dtype, hipStream_t st) {
   if (a.batch == 0) return hipSuccess;
-  if (a.key_stride > a.budget) {   // (else every row fits the budget)
-    switch (dtype) {
-      case 0: run_scores<Bf16, false>(a, st); break;
-      case 1: run_scores<Fp16, false>(a, st); break;
-      case 3: run_scores<Fp16, true>(a, st); break;
-      default: return hipErrorInvalidValue;
-    }
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+  switch (dtype) {
+    case 0: return run_typed<Bf16, false>(a, st);
+    case 1: return run_typed<Fp16, false>(a, st);
+    case 3: return run_typed<Fp16, true>(a, st);
+    default: return hipErrorInvalidValue;
   }
-  hipLaunchKernelGGL(select_kernel, dim3((unsigned)(a.batch * a.num_kv_heads)), dim3(64 * kSelectWaves), 0, st, a);
-  return hipGetLastError();
 }
 
 }  // namespace ekv

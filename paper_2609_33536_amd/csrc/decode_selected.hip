@@ -14,6 +14,7 @@
 // that the products read them from; the head-dim order of the QK product is free, as long as
 // Q follows it, and is chosen so that a wave's loads cover whole 128-byte lines.
 #include <algorithm>
+#include <type_traits>
 
 #include "attn_device.h"
 #include "common.h"
@@ -23,6 +24,7 @@ namespace ekv {
 namespace {
 
 constexpr int kTeam = 4;        // waves of a workgroup
+constexpr int kMostPieces = 64;
 constexpr float kLowest = -3.0e38f;   // reference maximum before the first score: finite, so that -inf scores weigh 0
 
 // One step's K and V as loaded: 16-bit pools 4 + 4 loads of 16 bytes a block, 8-bit ones
@@ -43,20 +45,25 @@ struct LaneOffsets {
   uint32_t k_target, v_target, k_base, v_base;
 };
 
-// 16-bit pools: lane (n, g) holds for QK step k the 8 elements of chunk
-// 2 g + 8 (k / 2) + k % 2 of token n, so that the steps' loads in pairs cover 128 bytes of a
-// row, and a BASE row's 16 bytes are two steps.  8-bit pools: chunk 4 g + k (a BASE row's 16 bytes
-// are all four).  V: tokens 4 g + i, elements 8 n .. 8 n + 7.
+// QK step k of lane (n, g) takes 8 elements of token n: of 16-bit pools chunk 4 k + g, so that a load covers 64 bytes of a
+// row; of 8-bit ones, where a load of 16 bytes is two steps, chunk 8 (k / 2) + 2 g + k % 2, to the same end.
+// V: tokens 4 g + i, elements 8 n .. 8 n + 7.  BASE rows are half as long: a load takes the 16 (8-bit V: 8) bytes that hold
+// the lane's half as much.
+template <bool F8>
+__device__ __forceinline__ constexpr int chunk_of(int g, int k) { return F8 ? 8 * (k >> 1) + 2 * g + (k & 1) : 4 * k + g; }
 template <bool F8>
 __device__ __forceinline__ LaneOffsets lane_offsets(int n, int g) {
   if constexpr (F8)
-    return {(uint32_t)(n * kHeadDim + 32 * g), (uint32_t)(4 * g * kHeadDim + 8 * n), (uint32_t)(n * kHeadDim / 2 + 16 * g),
+    return {(uint32_t)(n * kHeadDim + 16 * g), (uint32_t)(4 * g * kHeadDim + 8 * n), (uint32_t)(n * kHeadDim / 2 + (8 * g & ~15)),
             (uint32_t)(4 * g * kHeadDim / 2 + (4 * n & ~7))};
   else
-    return {(uint32_t)(n * 2 * kHeadDim + 32 * g), (uint32_t)(4 * g * 2 * kHeadDim + 16 * n), (uint32_t)(n * kHeadDim + 16 * g),
+    return {(uint32_t)(n * 2 * kHeadDim + 16 * g), (uint32_t)(4 * g * 2 * kHeadDim + 16 * n), (uint32_t)(n * kHeadDim + (8 * g & ~15)),
             (uint32_t)(4 * g * kHeadDim + (8 * n & ~15))};
 }
 
+// V is read past the caches, K is not: two loads of a wave take the halves of each of K's 128-byte lines, and a
+// line read past the first-level cache would come from the second twice.  (64 sequences of 2048 selected tokens, 32 / 8 heads, a quarter
+// BASE: 77.5 us; both past the caches 81.6, both through them 84.0.)
 template <typename V>
 __device__ __forceinline__ V once(const char* p, uint32_t off) {
   return __builtin_nontemporal_load(reinterpret_cast<const V*>(p + off));
@@ -65,23 +72,14 @@ __device__ __forceinline__ V once(const char* p, uint32_t off) {
 // kt, vt: the block's tiles (of its member, for BASE)
 template <bool F8, bool ELASTIC>
 __device__ __forceinline__ void load_block(Raw<F8>& r, const char* kt, const char* vt, bool base, const LaneOffsets& o) {
-  const uint32_t ko = ELASTIC && base ? o.k_base : o.k_target, vo = ELASTIC && base ? o.v_base : o.v_target;
-  if constexpr (F8) {
-    r.k[0] = once<u32x4>(kt, ko);
-    r.k[1] = once<u32x4>(kt, ko + (ELASTIC && base ? 0 : 16));
-    const uint32_t row = ELASTIC && base ? kHeadDim / 2 : kHeadDim;
+  const bool half = ELASTIC && base;
+  const uint32_t ko = half ? o.k_base : o.k_target, vo = half ? o.v_base : o.v_target;
+  constexpr uint32_t kRowBytes = F8 ? kHeadDim : 2 * kHeadDim;
+  const uint32_t step = half ? 32 : 64, row = half ? kRowBytes / 2 : kRowBytes;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) r.v[i] = once<u32x2>(vt, vo + i * row);
-  } else {
-    const uint32_t odd = ELASTIC && base ? 0 : 16, high = ELASTIC && base ? 64 : 128;
-    r.k[0] = once<u32x4>(kt, ko);
-    r.k[1] = once<u32x4>(kt, ko + odd);
-    r.k[2] = once<u32x4>(kt, ko + high);
-    r.k[3] = once<u32x4>(kt, ko + high + odd);
-    const uint32_t row = ELASTIC && base ? kHeadDim : 2 * kHeadDim;
+  for (int k = 0; k < (F8 ? 2 : 4); ++k) r.k[k] = *reinterpret_cast<const u32x4*>(kt + (ko + k * step));
 #pragma unroll
-    for (int i = 0; i < 4; ++i) r.v[i] = once<u32x4>(vt, vo + i * row);
-  }
+  for (int i = 0; i < 4; ++i) r.v[i] = once<std::remove_reference_t<decltype(r.v[i])>>(vt, vo + i * row);
 }
 
 // 8 bytes or 8 nibbles -> the executed FP16 words, in the order of the elements.
@@ -94,31 +92,31 @@ __device__ __forceinline__ u32x4 nibble_words(uint32_t w) {
 
 // Scores of a block's 16 tokens, and its V rows as 16-bit words.
 template <typename T, bool F8, bool ELASTIC>
-__device__ __forceinline__ void open_block(const Raw<F8>& r, bool base, const u32x4 (&q)[4], int n, f32x4& s, u32x4 (&v)[4]) {
+__device__ __forceinline__ void open_block(const Raw<F8>& r, bool base, const u32x4 (&q)[4], int n, int g, f32x4& s, u32x4 (&v)[4]) {
   s = f32x4{0.f, 0.f, 0.f, 0.f};
-  if constexpr (F8) {
-    if (ELASTIC && base) {
+  if (ELASTIC && base) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) s = Mma<T>::qk(nibble_words(r.k[0][k]), q[k], s);
+    for (int k = 0; k < 4; ++k) {
+      const u32x4 w = r.k[F8 ? k >> 1 : k];
+      const u32x2 mine = g & 1 ? w.zw : w.xy;
+      if constexpr (F8) s = Mma<T>::qk(nibble_words(k & 1 ? mine.y : mine.x), q[k], s);
+      else s = Mma<T>::qk(expand_base8(mine), q[k], s);
+    }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = nibble_words(n & 1 ? r.v[i].y : r.v[i].x);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) s = Mma<T>::qk(byte_words(k & 1 ? r.k[k >> 1].zw : r.k[k >> 1].xy), q[k], s);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = byte_words(r.v[i]);
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (F8) v[i] = nibble_words(n & 1 ? r.v[i].y : r.v[i].x);
+      else v[i] = expand_base8(n & 1 ? r.v[i].zw : r.v[i].xy);
     }
   } else {
-    if (ELASTIC && base) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) s = Mma<T>::qk(expand_base8(k & 1 ? r.k[k & 2].zw : r.k[k & 2].xy), q[k], s);
+    for (int k = 0; k < 4; ++k) {
+      if constexpr (F8) s = Mma<T>::qk(byte_words(k & 1 ? r.k[k >> 1].zw : r.k[k >> 1].xy), q[k], s);
+      else s = Mma<T>::qk(r.k[k], q[k], s);
+    }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = expand_base8(n & 1 ? r.v[i].zw : r.v[i].xy);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) s = Mma<T>::qk(r.k[k], q[k], s);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = r.v[i];
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (F8) v[i] = byte_words(r.v[i]);
+      else v[i] = r.v[i];
     }
   }
 }
@@ -179,13 +177,35 @@ __device__ __forceinline__ void softmax_step(SplitState& st, const f32x4 (&s)[2]
   }
 }
 
-__device__ __forceinline__ void store_agent2(float* p, float a, float b) {
-  const uint64_t v = (uint64_t)__float_as_uint(a) | ((uint64_t)__float_as_uint(b) << 32);
-  __hip_atomic_store(reinterpret_cast<uint64_t*>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+// Partials pass between workgroups with the agent-scope cache policy (sc1: written through to, and read
+// from, the memory side, which every XCD sees), through descriptors of the row's partials.
+constexpr int kAgentScope = 16;   // the sc1 bit of the cache-policy operand
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t partials(float* p, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(p, 0, bytes, 0x00020000);
 }
-__device__ __forceinline__ float2 load_agent2(const float* p) {
-  const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
+__device__ __forceinline__ f32x4 load_agent4(__amdgpu_buffer_rsrc_t r, uint32_t byte) {
+  return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, byte, 0, kAgentScope));
+}
+__device__ __forceinline__ float2 load_agent2(__amdgpu_buffer_rsrc_t r, uint32_t byte) {
+  return __builtin_bit_cast(float2, __builtin_amdgcn_raw_buffer_load_b64(r, byte, 0, kAgentScope));
+}
+
+// max / sum over the 16 lanes of a row
+template <int N>
+__device__ __forceinline__ float ror(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + N, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float row_max(float x) {
+  x = fmaxf(x, ror<8>(x));
+  x = fmaxf(x, ror<4>(x));
+  x = fmaxf(x, ror<2>(x));
+  return fmaxf(x, ror<1>(x));
+}
+__device__ __forceinline__ float row_sum(float x) {
+  x += ror<8>(x);
+  x += ror<4>(x);
+  x += ror<2>(x);
+  return x + ror<1>(x);
 }
 
 // LDS rows of 132 floats: the rows of 16 heads start 4 banks apart
@@ -193,8 +213,22 @@ constexpr int kRow = kHeadDim + 4;
 template <int G> struct Joined {
   float o[kTeam][G][kRow];
   float m[kTeam][G], l[kTeam][G];
+  float weight[kMostPieces][G], inv[G];
+  f32x4 part[64 * kTeam];
   int last;
 };
+
+template <typename T>
+__device__ __forceinline__ void store_chunk(void* out, size_t at, f32x4 x, bool fp32) {
+  if (fp32) {
+    *reinterpret_cast<f32x4*>(static_cast<float*>(out) + at) = x;
+  } else {
+    float back;
+    *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(out) + at) =
+        u32x2{(uint32_t)Mma<T>::round(x[0], &back) | ((uint32_t)Mma<T>::round(x[1], &back) << 16),
+              (uint32_t)Mma<T>::round(x[2], &back) | ((uint32_t)Mma<T>::round(x[3], &back) << 16)};
+  }
+}
 
 template <typename T, int G, bool ELASTIC, bool F8>
 __global__ __launch_bounds__(64 * kTeam, 2) void selected_kernel(SelectedArgs a) {
@@ -236,10 +270,11 @@ __global__ __launch_bounds__(64 * kTeam, 2) void selected_kernel(SelectedArgs a)
     if ((unsigned)i < (unsigned)blocks) {
       const size_t at = (size_t)s * b.max_blocks + i;
       const int block = b.bt[at];
+      const uint8_t tag = (by_tags ? b.tags : reinterpret_cast<const uint8_t*>(b.bt))[at];   // (one round trip)
       phys = (unsigned)block < (unsigned)b.num_blocks ? block : 0;   // never leave the pool
       mode = min(kPage, len - i * kPage) | (i & 1) << 8;
       if constexpr (ELASTIC)
-        if (by_tags ? b.tags[at] != 0 : (i >= base_lo && i < base_hi)) mode |= 1 << 9;
+        if (by_tags ? tag != 0 : (i >= base_lo && i < base_hi)) mode |= 1 << 9;
     }
   };
 
@@ -249,12 +284,8 @@ __global__ __launch_bounds__(64 * kTeam, 2) void selected_kernel(SelectedArgs a)
   u32x4 q[4];
   const size_t head0 = (size_t)s * a.num_q_heads + (size_t)kvh * G;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const int chunk = F8 ? 4 * g + k : 2 * g + 8 * (k >> 1) + (k & 1);
-    q[k] = u32x4{0u, 0u, 0u, 0u};
-    if (n < (kStack ? 2 * G : G))
-      q[k] = *reinterpret_cast<const u32x4*>(a.q + (head0 + n % G) * kHeadDim + 8 * chunk) ^ sign;
-  }
+  for (int k = 0; k < 4; ++k)
+    q[k] = *reinterpret_cast<const u32x4*>(a.q + (head0 + n % G) * kHeadDim + 8 * chunk_of<F8>(g, k));
 
   SplitState st;
 #pragma unroll
@@ -269,6 +300,9 @@ __global__ __launch_bounds__(64 * kTeam, 2) void selected_kernel(SelectedArgs a)
   // Windows of 64 entries (32 steps); a window's entries are fetched while the one before is worked on.
   int phys, mode, phys_next = 0, mode_next = 0;
   fetch(2 * first, phys, mode);
+  const bool used = n < (kStack ? 2 * G : G);   // (the queries' loads are on their way beside the list's)
+#pragma unroll
+  for (int k = 0; k < 4; ++k) q[k] = used ? q[k] ^ sign : u32x4{0u, 0u, 0u, 0u};
   for (int w0 = first; w0 < last; w0 += 32) {
     fetch(2 * (w0 + 32), phys_next, mode_next);
     const int here = min(32, last - w0);
@@ -295,8 +329,8 @@ __global__ __launch_bounds__(64 * kTeam, 2) void selected_kernel(SelectedArgs a)
         if (t + d < here && ((m0 | m1) & 255)) {
           f32x4 sc[2];
           u32x4 v[2][4];
-          open_block<T, F8, ELASTIC>(raw[d][0], m0 & (1 << 9), q, n, sc[0], v[0]);
-          open_block<T, F8, ELASTIC>(raw[d][1], m1 & (1 << 9), q, n, sc[1], v[1]);
+          open_block<T, F8, ELASTIC>(raw[d][0], m0 & (1 << 9), q, n, g, sc[0], v[0]);
+          open_block<T, F8, ELASTIC>(raw[d][1], m1 & (1 << 9), q, n, g, sc[1], v[1]);
           softmax_step<T, G>(st, sc, v, m0 & 255, m1 & 255, scale, g, n);
         }
         load(raw[d], t + d + kDepth);
@@ -322,27 +356,33 @@ __global__ __launch_bounds__(64 * kTeam, 2) void selected_kernel(SelectedArgs a)
     }
   }
   __syncthreads();
-  float* const part_o = a.ws_o + ((size_t)row * a.pieces + piece) * G * kHeadDim;
-  float* const part_ml = a.ws_ml + ((size_t)row * a.pieces + piece) * G * 2;
-  for (int e = threadIdx.x; e < G * kHeadDim / 2; e += 64 * kTeam) {
-    const int h = e / (kHeadDim / 2), d = 2 * (e % (kHeadDim / 2));
+  constexpr int kChunks = G * kHeadDim / 4, kAll = 64 * kTeam;   // 16-byte chunks of the group's output
+  constexpr uint32_t kSlot = G * kHeadDim * sizeof(float), kSlotMl = G * 2 * sizeof(float);
+  const auto part_o = partials(a.ws_o + (size_t)row * a.pieces * G * kHeadDim, a.pieces * kSlot);
+  const auto part_ml = partials(a.ws_ml + (size_t)row * a.pieces * G * 2, a.pieces * kSlotMl);
+#pragma unroll
+  for (int c = 0; c < (kChunks + kAll - 1) / kAll; ++c) {
+    const int e = c * kAll + (int)threadIdx.x, h = e / (kHeadDim / 4), d = 4 * (e % (kHeadDim / 4));
+    if (kChunks < kAll && e >= kChunks) break;
     float m = sm.m[0][h];
 #pragma unroll
     for (int w = 1; w < kTeam; ++w) m = fmaxf(m, sm.m[w][h]);
-    float sum = 0.f, x = 0.f, y = 0.f;
+    float sum = 0.f;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < kTeam; ++w) {
       const float f = fast_exp2(sm.m[w][h] - m);
       sum = fmaf(f, sm.l[w][h], sum);
-      x = fmaf(f, sm.o[w][h][d], x);
-      y = fmaf(f, sm.o[w][h][d + 1], y);
+      x += f * *reinterpret_cast<const f32x4*>(&sm.o[w][h][d]);
     }
     if (a.pieces == 1) {
       const float inv = sum == 0.f ? 0.f : 1.0f / sum;   // (no token: zeros)
-      store_pair<T>(a.out, (head0 + h) * kHeadDim + d, x * inv, y * inv, a.out_fp32);
+      store_chunk<T>(a.out, (head0 + h) * kHeadDim + d, x * inv, a.out_fp32);
     } else {
-      store_agent2(part_o + h * kHeadDim + d, x, y);
-      if (d == 0) store_agent2(part_ml + 2 * h, m, sum);
+      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), part_o, piece * kSlot + 16 * e, 0, kAgentScope);
+      if (d == 0)
+        __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, make_float2(m, sum)), part_ml, piece * kSlotMl + 8 * h, 0,
+                                              kAgentScope);
     }
   }
   if (a.pieces == 1) return;
@@ -358,22 +398,67 @@ __global__ __launch_bounds__(64 * kTeam, 2) void selected_kernel(SelectedArgs a)
   __syncthreads();
   if (!sm.last) return;
   asm volatile("" ::: "memory");
-  const float* const all_o = a.ws_o + (size_t)row * a.pieces * G * kHeadDim;
-  const float* const all_ml = a.ws_ml + (size_t)row * a.pieces * G * 2;
-  for (int e = threadIdx.x; e < G * kHeadDim / 2; e += 64 * kTeam) {
-    const int h = e / (kHeadDim / 2), d = 2 * (e % (kHeadDim / 2));
-    float m = kLowest;
-    for (int p = 0; p < a.pieces; ++p) m = fmaxf(m, load_agent2(all_ml + 2 * (p * G + h)).x);
-    float sum = 0.f, x = 0.f, y = 0.f;
-    for (int p = 0; p < a.pieces; ++p) {
-      const float2 ml = load_agent2(all_ml + 2 * (p * G + h)), o = load_agent2(all_o + (size_t)(p * G + h) * kHeadDim + d);
-      const float f = fast_exp2(ml.x - m);
-      sum = fmaf(f, ml.y, sum);
-      x = fmaf(f, o.x, x);
-      y = fmaf(f, o.y, y);
+  // Thread e holds chunk e (groups of 16 heads: and e + 256) of the pieces r, r + kShares, ..; the
+  // first of them are on their way while the weights are worked out.  Past the last piece: beyond the descriptor's
+  // bound, which reads zeros and no memory.
+  constexpr int kShares = kChunks < kAll ? kAll / kChunks : 1, kHeld = kChunks > kAll ? kChunks / kAll : 1, kAhead = 16 / kHeld;
+  const int e = threadIdx.x % kChunks, r = threadIdx.x / kChunks;
+  f32x4 v[kAhead][kHeld];
+  auto load = [&](int k0) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int p = r + (k0 + u) * kShares;
+#pragma unroll
+      for (int c = 0; c < kHeld; ++c) v[u][c] = load_agent4(part_o, p < a.pieces ? p * kSlot + 16 * (e + c * kAll) : 0x80000000u);
     }
-    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-    store_pair<T>(a.out, (head0 + h) * kHeadDim + d, x * inv, y * inv, a.out_fp32);
+  };
+  load(0);
+  if (threadIdx.x < 16 * G) {   // 16 lanes a head, 4 pieces a lane
+    const int h = threadIdx.x / 16, j = threadIdx.x % 16;
+    float2 ml[kMostPieces / 16];
+#pragma unroll
+    for (int u = 0; u < kMostPieces / 16; ++u)
+      ml[u] = j + 16 * u < a.pieces ? load_agent2(part_ml, (j + 16 * u) * kSlotMl + 8 * h) : make_float2(kLowest, 0.f);
+    float m = ml[0].x;
+#pragma unroll
+    for (int u = 1; u < kMostPieces / 16; ++u) m = fmaxf(m, ml[u].x);
+    m = row_max(m);
+    float sum = 0.f;
+#pragma unroll
+    for (int u = 0; u < kMostPieces / 16; ++u) {
+      const float f = fast_exp2(ml[u].x - m);
+      sum = fmaf(f, ml[u].y, sum);
+      sm.weight[j + 16 * u][h] = f;
+    }
+    sum = row_sum(sum);
+    if (j == 0) sm.inv[h] = sum == 0.f ? 0.f : 1.0f / sum;
+  }
+  __syncthreads();
+  f32x4 x[kHeld];
+#pragma unroll
+  for (int c = 0; c < kHeld; ++c) x[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+  for (int k0 = 0; r + k0 * kShares < a.pieces; k0 += kAhead) {
+    if (k0 > 0) load(k0);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int p = r + (k0 + u) * kShares;
+      if (p < a.pieces)
+#pragma unroll
+        for (int c = 0; c < kHeld; ++c) x[c] += sm.weight[p][(e + c * kAll) / (kHeadDim / 4)] * v[u][c];
+    }
+  }
+  if constexpr (kShares > 1) {
+    sm.part[threadIdx.x] = x[0];
+    __syncthreads();
+    if (r > 0) return;
+#pragma unroll
+    for (int k = 1; k < kShares; ++k) x[0] += sm.part[e + k * kChunks];
+  }
+#pragma unroll
+  for (int c = 0; c < kHeld; ++c) {
+    const int at = e + c * kAll, h = at / (kHeadDim / 4);
+    store_chunk<T>(a.out, (head0 + h) * kHeadDim + 4 * (at % (kHeadDim / 4)), x[c] * sm.inv[h], a.out_fp32);
   }
 }
 
@@ -400,9 +485,9 @@ hipError_t run_group(const SelectedArgs& a, int group, bool elastic, hipStream_t
 }  // namespace
 
 int selected_pieces(int64_t rows, int budget) {
-  // 512 workgroups fill the chip (two a compute unit); a wave takes at least one step of two blocks
-  const int64_t wanted = (512 + rows - 1) / std::max<int64_t>(rows, 1), most = (budget + 2 * kTeam - 1) / (2 * kTeam);
-  return (int)std::max<int64_t>(1, std::min(wanted, most));
+  // 512 workgroups fill the chip (two a compute unit); a wave takes two steps of two blocks or more
+  const int64_t wanted = (512 + rows - 1) / std::max<int64_t>(rows, 1), most = (budget + 4 * kTeam - 1) / (4 * kTeam);
+  return (int)std::max<int64_t>(1, std::min<int64_t>({wanted, most, kMostPieces}));
 }
 
 hipError_t launch_selected(const SelectedArgs& a, int dtype, int group, bool elastic, hipStream_t st) {

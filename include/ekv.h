@@ -793,7 +793,7 @@ ekv_status ekv_attn_decode_shared(const ekv_pool* pool, const ekv_batch* prefixe
  * pairs: a later call with known[s] at or before them refreshes the bounds.  (Bounds
  * from before it only make the scores of those blocks less tight or less sure.)
  * Errors: as ekv_attn_decode; EKV_ERR_UNSUPPORTED also for more than 2^22 rows (batch
- * times KV heads).
+ * times KV heads), or 2^31 pairs of blocks over all rows.
  */
 ekv_status ekv_key_bounds(const ekv_pool* pool, const ekv_batch* batch, const int32_t* known, void* bounds,
                           hipStream_t stream);
@@ -813,9 +813,9 @@ ekv_status ekv_key_bounds(const ekv_pool* pool, const ekv_batch* batch, const in
  *   selected  device int32 [batch][num_kv_heads][budget]: the logical blocks in
  *             ascending order, then -1
  *   counts    device int32 [batch][num_kv_heads]: min(n, budget)
- *   ws        device scratch of ekv_select_workspace_bytes() bytes, 16-byte aligned,
- *             prepared by ekv_decode_workspace_init (or zero-filled) before its first
- *             use; calls that share one must be ordered
+ *   ws        device scratch of ekv_select_workspace_bytes() bytes (of one size for
+ *             all sink and recent), 16-byte aligned; needs no preparation and keeps
+ *             nothing between calls; calls that share one must be ordered
  * 0 <= sink, recent; sink + recent <= budget < 2^20.  Of the pool only its shape and of the
  * batch its lengths and sizes are used.
  * Errors: as ekv_key_bounds; EKV_ERR_INVALID also for the budget, sink and recent, and

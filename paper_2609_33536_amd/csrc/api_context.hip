@@ -98,22 +98,28 @@ SelectedLayout selected_layout(const ekv_pool* pool, const ekv_batch* b, int32_t
   return l;
 }
 
-// EKV_DEBUG: a block that a list names twice.
+// EKV_DEBUG: a block of its sequence that a list names twice.
 ekv_status debug_check_lists(const ekv_pool* pool, const ekv_batch* b, const int32_t* selected, const int32_t* counts,
                              int32_t budget, hipStream_t stream) {
   const size_t rows = (size_t)b->batch * pool->num_kv_heads;
-  std::vector<int32_t> list(rows * budget), n(rows, budget);
-  hipError_t e = hipMemcpyAsync(list.data(), selected, list.size() * sizeof(int32_t), hipMemcpyDeviceToHost, stream);
-  if (e == hipSuccess && counts) e = hipMemcpyAsync(n.data(), counts, rows * sizeof(int32_t), hipMemcpyDeviceToHost, stream);
+  std::vector<int32_t> list(rows * budget), n(rows, budget), lens(b->batch);
+  auto read = [&](std::vector<int32_t>& to, const int32_t* from) {
+    return hipMemcpyAsync(to.data(), from, to.size() * sizeof(int32_t), hipMemcpyDeviceToHost, stream);
+  };
+  hipError_t e = read(list, selected);
+  if (e == hipSuccess) e = read(lens, b->seq_lens);
+  if (e == hipSuccess && counts) e = read(n, counts);
   if (e == hipSuccess) e = hipStreamSynchronize(stream);
   if (e != hipSuccess) return hip_status(e, "ekv_attn_decode_selected (EKV_DEBUG)");
   for (size_t r = 0; r < rows; ++r) {
-    const auto begin = list.begin() + r * budget, end = begin + std::min(std::max(n[r], 0), budget);
+    const int s = (int)(r / pool->num_kv_heads), blocks = (lens[s] + kPage - 1) / kPage;   // (lengths are checked before)
+    const auto begin = list.begin() + r * budget;
+    const auto end = std::remove_if(begin, begin + std::min(std::max(n[r], 0), budget), [&](int32_t i) { return i < 0 || i >= blocks; });
     std::sort(begin, end);
-    const auto twice = std::adjacent_find(std::lower_bound(begin, end, 0), end);
+    const auto twice = std::adjacent_find(begin, end);
     if (twice != end)
       return fail(EKV_ERR_INVALID, "ekv_attn_decode_selected (EKV_DEBUG): block %d is listed twice for sequence %d, KV head %d",
-                  *twice, (int)(r / pool->num_kv_heads), (int)(r % pool->num_kv_heads));
+                  *twice, s, (int)(r % pool->num_kv_heads));
   }
   return EKV_OK;
 }

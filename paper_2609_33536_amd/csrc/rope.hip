@@ -125,8 +125,8 @@ __device__ __forceinline__ void level(const RopeArgs& a, float (&x)[8], float (&
   floats8<T>(w1, v);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    x[i] *= weighted ? f * (u[i] + a.offset) : f;
-    y[i] *= weighted ? f * (v[i] + a.offset) : f;
+    x[i] = x[i] * f * (weighted ? u[i] + a.offset : 1.0f);   // (x f is at most the root of 128)
+    y[i] = y[i] * f * (weighted ? v[i] + a.offset : 1.0f);
   }
 }
 

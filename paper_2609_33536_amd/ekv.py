@@ -633,11 +633,10 @@ def key_bounds(pool, batch, bounds, known=None, stream=None):
                                 _bounds_ptr(pool, batch, bounds), _stream(stream)))
 
 
-def _workspace(nbytes, device):
-    import torch
-    if nbytes == 0:
+def _workspace(nbytes):
+    if nbytes == 0:   # (refused: the library has said why)
         raise EkvError(ERR_INVALID, lib().ekv_last_error().decode())
-    return torch.zeros(nbytes, dtype=torch.uint8, device=device)
+    return nbytes
 
 
 def select_workspace_bytes(pool, batch, budget):
@@ -645,8 +644,9 @@ def select_workspace_bytes(pool, batch, budget):
 
 
 def select_workspace(pool, batch, budget, device="cuda"):
-    """A zero-filled workspace for :func:`select_blocks`."""
-    return _workspace(select_workspace_bytes(pool, batch, budget), device)
+    """Scratch for :func:`select_blocks` (it needs no preparation)."""
+    import torch
+    return torch.empty(_workspace(select_workspace_bytes(pool, batch, budget)), dtype=torch.uint8, device=device)
 
 
 def select_blocks(pool, batch, q, bounds, selected, counts, ws, sink=1, recent=1, stream=None):
@@ -672,7 +672,8 @@ def decode_selected_workspace_bytes(pool, batch, budget):
 
 def decode_selected_workspace(pool, batch, budget, device="cuda"):
     """A zero-filled workspace for :func:`attn_decode_selected` (its merge counters start at zero)."""
-    return _workspace(decode_selected_workspace_bytes(pool, batch, budget), device)
+    import torch
+    return torch.zeros(_workspace(decode_selected_workspace_bytes(pool, batch, budget)), dtype=torch.uint8, device=device)
 
 
 def attn_decode_selected(pool, batch, selected, counts, q, out, scale, ws, stream=None):

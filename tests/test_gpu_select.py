@@ -47,7 +47,9 @@ class Rows:
         b = len(self.lens)
         out = torch.full((b + 1, self.hkv, budget), 12345, dtype=torch.int32, device="cuda")
         counts = torch.full((b, self.hkv), -7, dtype=torch.int32, device="cuda")
-        ws = ekv.select_workspace(self.pool, self.batch, budget) if ws is None else ws
+        if ws is None:
+            ws = ekv.select_workspace(self.pool, self.batch, budget)
+            ws.fill_(0xFF)   # (nothing of it may matter)
         ekv.select_blocks(self.pool, self.batch, self.d_q, self.d_bounds, out[:b], counts, ws, sink, recent, stream)
         torch.cuda.synchronize()
         assert (out[b] == 12345).all()

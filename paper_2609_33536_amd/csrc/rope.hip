@@ -14,6 +14,12 @@
 // by HBM: q in and out, k and v in, their cache rows out.  16384 tokens of 64 + 2 x 8 heads
 // into an 8-bit pool, not in a cache, take 128 us (638 MB, 5.0 TB/s; a plain copy reaches
 // 5.2), 64 tokens of 32 + 2 x 8 heads 4.4 us (a launch).
+//
+// Heads may be levelled first (the norms of queries and keys): x / sqrt(mean(x^2) + eps) (offset +
+// weight) in the same registers, the squares summed over the 8 lanes, so that a norm adds no byte but
+// its weights.  16384 tokens of 64 + 2 x 8 heads into an 8-bit pool take 129 us with norms as without;
+// 8192 of 32 + 2 x 8 into a 16-bit one 43 (38.5 without: its vector work, 350 instructions a
+// wave and 8 rows, is as long as its loads and stores and not all hidden), 64 5.1.
 #include <algorithm>
 
 #include "common.h"
@@ -58,14 +64,16 @@ __device__ __forceinline__ void cos_sin(uint64_t p, float m, float& c, float& s)
 }
 
 // 8 floats -> 8 words of T (to nearest) or, for an 8-bit pool, 8 E5M2 bytes (to nearest, straight from 32 bits)
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+template <typename T> struct Pair;
+template <> struct Pair<Bf16> { typedef __bf16 two __attribute__((ext_vector_type(2))); };
+template <> struct Pair<Fp16> { typedef _Float16 two __attribute__((ext_vector_type(2))); };
 template <typename T>
 __device__ __forceinline__ u32x4 words8(const float (&x)[8]) {
   u32x4 w;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float back;
-    w[i] = (uint32_t)Mma<T>::round(x[2 * i], &back) | ((uint32_t)Mma<T>::round(x[2 * i + 1], &back) << 16);
-  }
+  for (int i = 0; i < 4; ++i)
+    w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x[2 * i], x[2 * i + 1]}), typename Pair<T>::two));
   return w;
 }
 __device__ __forceinline__ u32x2 bytes8(const float (&x)[8]) {
@@ -106,8 +114,7 @@ __device__ __forceinline__ float squares(const float (&x)[8], const float (&y)[8
 // A head's elements times 1 / sqrt(mean of their squares + eps) and the weights.  Squares
 // are summed in 32 bits; where that overflows (bf16 values beyond 10^18), over elements
 // 2^-70 as large, whose squares are far above any eps that was not lost before.
-template <typename T>
-__device__ __forceinline__ void level(const RopeArgs& a, float (&x)[8], float (&y)[8], bool weighted, u32x4 w0, u32x4 w1) {
+__device__ __forceinline__ void level(const RopeArgs& a, float (&x)[8], float (&y)[8], const float (&u)[8], const float (&v)[8]) {
   constexpr float kDown = 0x1p-70f;
   float sum = squares(x, y), eps = a.eps;
   if (!(sum < __builtin_inff())) {
@@ -120,18 +127,18 @@ __device__ __forceinline__ void level(const RopeArgs& a, float (&x)[8], float (&
     eps = 0.0f;
   }
   const float f = __builtin_amdgcn_rsqf(fmaf(sum, 1.0f / kHeadDim, eps));
-  float u[8], v[8];
-  floats8<T>(w0, u);
-  floats8<T>(w1, v);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    x[i] = x[i] * f * (weighted ? u[i] + a.offset : 1.0f);   // (x f is at most the root of 128)
-    y[i] = y[i] * f * (weighted ? v[i] + a.offset : 1.0f);
+    x[i] = x[i] * f * u[i];   // (x f is at most the root of 128)
+    y[i] = y[i] * f * v[i];
   }
 }
 
-// ONCE: inputs are read past the caches.  NORM: query and key heads are levelled first
-template <typename T, bool F8, bool ONCE, bool NORM>
+// Norms: none; by weights that all heads share (or none), kept in registers; by weights read for each row.
+enum Norm { kNoNorm, kShared, kPerHead };
+
+// ONCE: inputs are read past the caches
+template <typename T, bool F8, bool ONCE, int NORM>
 __global__ __launch_bounds__(64 * kWaves) void rope_kernel(RopeArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 7;
   const int rows = a.num_q_heads + 2 * a.num_kv_heads;   // rows of a token: query heads, key heads, value heads
@@ -147,13 +154,24 @@ __global__ __launch_bounds__(64 * kWaves) void rope_kernel(RopeArgs a) {
   const int chunk0 = a.pairs ? 2 * c : (c < turned ? c : 2 * turned + 2 * (c - turned));
   const int chunk1 = a.pairs ? 2 * c + 1 : (c < turned ? turned + c : chunk0 + 1);
   const int values0 = a.num_q_heads + a.num_kv_heads;              // the first value head
-  auto load_weights = [&](int r, u32x4& w0, u32x4& w1) {   // (the same few rows for every token: from the caches)
-    const bool key = r >= a.num_q_heads;
-    const uint16_t* src = key ? a.k_weight : a.q_weight;
-    if (!src || r >= values0) return;
-    src += key ? (r - a.num_q_heads) * a.k_weight_stride : r * a.q_weight_stride;
-    w0 = *reinterpret_cast<const u32x4*>(src + 8 * chunk0);
-    w1 = *reinterpret_cast<const u32x4*>(src + 8 * chunk1);
+  // Weights of this lane's elements: as loaded (row r's head's; 0 for all heads'), and plus the offset, or 1.
+  auto load_weights = [&](const uint16_t* src, int head, int stride, u32x4& w0, u32x4& w1) {
+    if (!src) return;
+    w0 = *reinterpret_cast<const u32x4*>(src + head * stride + 8 * chunk0);
+    w1 = *reinterpret_cast<const u32x4*>(src + head * stride + 8 * chunk1);
+  };
+  auto weights = [&](const uint16_t* src, u32x4 w0, u32x4 w1, float (&u)[8], float (&v)[8]) {
+    floats8<T>(w0, u);
+    floats8<T>(w1, v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      u[i] = src ? u[i] + a.offset : 1.0f;
+      v[i] = src ? v[i] + a.offset : 1.0f;
+    }
+  };
+  auto load_head_weights = [&](int r, u32x4& w0, u32x4& w1) {
+    if (r < a.num_q_heads) load_weights(a.q_weight, r, a.q_weight_stride, w0, w1);
+    else if (r < values0) load_weights(a.k_weight, r - a.num_q_heads, a.k_weight_stride, w0, w1);
   };
   auto load = [&](int r, u32x4& w0, u32x4& w1) {
     const uint16_t* src = r < a.num_q_heads ? a.q + token * a.q_stride + (size_t)r * kHeadDim
@@ -171,10 +189,14 @@ __global__ __launch_bounds__(64 * kWaves) void rope_kernel(RopeArgs a) {
   // (the first row's values are on their way while the angles are worked out, the next row's while one is turned)
   int r = row0 + (lane >> 3);
   u32x4 next0{0u, 0u, 0u, 0u}, next1{0u, 0u, 0u, 0u};
-  u32x4 weight0{0u, 0u, 0u, 0u}, weight1{0u, 0u, 0u, 0u};
+  u32x4 weight0{0u, 0u, 0u, 0u}, weight1{0u, 0u, 0u, 0u}, k_weight0{0u, 0u, 0u, 0u}, k_weight1{0u, 0u, 0u, 0u};
   if (r < row_end) {
     load(r, next0, next1);
-    if constexpr (NORM) load_weights(r, weight0, weight1);
+    if constexpr (NORM == kPerHead) load_head_weights(r, weight0, weight1);
+  }
+  if constexpr (NORM == kShared) {
+    load_weights(a.q_weight, 0, 0, weight0, weight1);
+    load_weights(a.k_weight, 0, 0, k_weight0, k_weight1);
   }
 
   const bool in_pool = slot >= 0 && slot / kPage < a.num_blocks;   // (outside the pool: the cache is left as it is)
@@ -186,22 +208,40 @@ __global__ __launch_bounds__(64 * kWaves) void rope_kernel(RopeArgs a) {
     if (c < turned) cos_sin((uint64_t)position * a.turns[8 * c + i], a.magnitude, cs[i], sn[i]);
   }
 
+  float qu[8], qv[8], ku[8], kv[8];
+  if constexpr (NORM == kShared) {
+    weights(a.q_weight, weight0, weight1, qu, qv);
+    weights(a.k_weight, k_weight0, k_weight1, ku, kv);
+  }
+
 #pragma unroll 1
   for (; r < row_end; r += 8) {
     u32x4 w0 = next0, w1 = next1;
     const u32x4 u0 = weight0, u1 = weight1;
     if (r + 8 < row_end) {
       load(r + 8, next0, next1);
-      if constexpr (NORM) load_weights(r + 8, weight0, weight1);
+      if constexpr (NORM == kPerHead) load_head_weights(r + 8, weight0, weight1);
     }
     const int kind = r < a.num_q_heads ? 0 : (r < values0 ? 1 : 2);   // query, key, value
     if (kind != 0 && !in_pool) continue;
     float x[8], y[8];
-    if (kind != 2 && (NORM || c < turned)) {
+    if (kind != 2 && (NORM != kNoNorm || c < turned)) {
       floats8<T>(w0, x);
       floats8<T>(w1, y);
-      if constexpr (NORM) level<T>(a, x, y, (kind == 0 ? a.q_weight : a.k_weight) != nullptr, u0, u1);
-      if (NORM && c >= turned) {
+      if constexpr (NORM != kNoNorm) {
+        float u[8], v[8];
+        if constexpr (NORM == kShared) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            u[i] = kind == 0 ? qu[i] : ku[i];
+            v[i] = kind == 0 ? qv[i] : kv[i];
+          }
+        } else {
+          weights(kind == 0 ? a.q_weight : a.k_weight, u0, u1, u, v);
+        }
+        level(a, x, y, u, v);
+      }
+      if (NORM != kNoNorm && c >= turned) {
         // (levelled, not turned)
       } else if (a.pairs) {   // elements 16 c + 2 i, + 1
 #pragma unroll
@@ -246,15 +286,18 @@ __global__ __launch_bounds__(64 * kWaves) void rope_kernel(RopeArgs a) {
   }
 }
 
-template <typename T, bool F8, bool NORM>
+template <typename T, bool F8, int NORM>
 void launch_once(const RopeArgs& a, dim3 grid, dim3 block, bool once, hipStream_t st) {
   if (once) hipLaunchKernelGGL((rope_kernel<T, F8, true, NORM>), grid, block, 0, st, a);
   else hipLaunchKernelGGL((rope_kernel<T, F8, false, NORM>), grid, block, 0, st, a);
 }
 template <typename T, bool F8>
 void launch_typed(const RopeArgs& a, dim3 grid, dim3 block, bool once, hipStream_t st) {
-  if (a.norm) launch_once<T, F8, true>(a, grid, block, once, st);
-  else launch_once<T, F8, false>(a, grid, block, once, st);
+  if (!a.norm) launch_once<T, F8, kNoNorm>(a, grid, block, once, st);
+  // (shared weights are worth keeping from 16 rows a wave on: 512 tokens of 32 / 8 heads 6.8 us, read a row 6.9, 2048 11.9 and
+  // 12.6; with 8 rows a wave, 64 tokens, 5.5 and 5.1)
+  else if (a.q_weight_stride == 0 && a.k_weight_stride == 0 && a.rows_per_wave > 8) launch_once<T, F8, kShared>(a, grid, block, once, st);
+  else launch_once<T, F8, kPerHead>(a, grid, block, once, st);
 }
 
 }  // namespace

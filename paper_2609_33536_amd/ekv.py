@@ -562,14 +562,15 @@ def make_head_norm(q_weight=None, k_weight=None, eps=1e-6, offset=0.0):
     (qp, qs), (kp, ks) = _head_weight(q_weight, "q_weight"), _head_weight(k_weight, "k_weight")
     norm = HeadNorm(qp, kp, qs, ks, eps, offset)
     norm.tensors = (q_weight, k_weight)   # (kept: the struct holds their addresses)
+    norm.kinds = [None if t is None else (t.dtype, None if t.dim() == 1 else t.shape[0]) for t in norm.tensors]
     return norm
 
 
 def norm_rope_append(pool, rope, norm, positions, slots, q, k, v, q_out, stream=None):
     """ekv_norm_rope_append: :func:`rope_append` with every query and key head
     levelled first (:func:`make_head_norm`)."""
-    for weight, x, name in zip(getattr(norm, "tensors", (None, None)), (q, k), ("q_weight", "k_weight")):
-        if weight is not None and (weight.dtype is not x.dtype or (weight.dim() == 2 and weight.shape[0] != x.shape[1])):
+    for kind, x, name in zip(norm.kinds, (q, k), ("q_weight", "k_weight")):
+        if kind is not None and (kind[0] is not x.dtype or kind[1] not in (None, x.shape[1])):
             raise EkvError(ERR_INVALID, f"{name} must be {x.dtype} [128] or [{x.shape[1]}][128]")
     _check(lib().ekv_norm_rope_append(ctypes.byref(pool), ctypes.byref(rope), ctypes.byref(norm),
                                       *_rope_arguments(pool, positions, slots, q, k, v, q_out), _stream(stream)))

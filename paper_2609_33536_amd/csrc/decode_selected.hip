@@ -484,10 +484,19 @@ hipError_t run_group(const SelectedArgs& a, int group, bool elastic, hipStream_t
 
 }  // namespace
 
+// A list is cut while its pieces stay within one workgroup a compute unit, where a piece has about 16 blocks
+// (a wave two steps) or more: a compute unit's four waves with two steps ahead nearly reach their share of the bandwidth,
+// and what a second workgroup there gains the join costs.  Measured in us, pieces up to 256 | up to 512 workgroups in all,
+// lists of 256 blocks half BASE, 8 KV heads: 16-bit 4 sequences 16.0 | 18.8, 8 22.4 | 32.7, 15 35.8 | 45.3;
+// 8-bit 8 sequences 17.5 | 33.7, 15 24.2 | 34.7.  (8 lists of 256 blocks in 4, 8, 16, 32 pieces: 17.1, 12.6, 10.9, 10.8.)
+// Lists of up to 32 blocks take less uncut (9.1, in two pieces 9.6).  A little above 256 lists some compute units
+// have two workgroups and most one: lists of 128 blocks or more are halved up to 384 of them (33 sequences
+// 103.6 -> 87.4, 8-bit 56.5 -> 53.3; 48: 109.6 -> 102.7, 62.6 -> 60.7; but 56: 114.9 -> 124.8, 67.2 -> 76.2).
 int selected_pieces(int64_t rows, int budget) {
-  // 512 workgroups fill the chip (two a compute unit); a wave takes two steps of two blocks or more
-  const int64_t wanted = (512 + rows - 1) / std::max<int64_t>(rows, 1), most = (budget + 4 * kTeam - 1) / (4 * kTeam);
-  return (int)std::max<int64_t>(1, std::min<int64_t>({wanted, most, kMostPieces}));
+  constexpr int kUnits = 256;
+  if (budget <= 32 || rows <= 0) return 1;
+  if (rows > kUnits) return rows <= kUnits * 3 / 2 && budget >= 128 ? 2 : 1;
+  return (int)std::min<int64_t>({kUnits / rows, (budget + 4 * kTeam - 1) / (4 * kTeam), kMostPieces});
 }
 
 hipError_t launch_selected(const SelectedArgs& a, int dtype, int group, bool elastic, hipStream_t st) {

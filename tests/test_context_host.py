@@ -161,13 +161,13 @@ def test_select_workspace_holds_what_any_first_and_newest_blocks_leave(lib, batc
         _refused(lib, lib.ekv_select_blocks(ctypes.byref(p), ctypes.byref(b), *dict(a, ws_bytes=size).values(), None), INVALID, "aligned")
 
 
-@pytest.mark.parametrize("batch,budget", [(1, 1), (1, 256), (1, 100000), (63, 128), (64, 128), (500, 16)])
-def test_decode_selected_workspace_sizes(lib, batch, budget):
+@pytest.mark.parametrize("batch,budget,pieces", [(1, 1, 1), (1, 32, 1), (1, 33, 3), (1, 256, 16), (1, 100000, 32), (16, 256, 2),
+                                                 (17, 256, 1), (32, 128, 1), (33, 127, 1), (33, 128, 2), (48, 128, 2),
+                                                 (49, 128, 1), (500, 16, 1)])
+def test_decode_selected_workspace_sizes(lib, batch, budget, pieces):
     p, b = _pool(), _batch(batch=batch)
     size = lib.ekv_decode_selected_workspace_bytes(ctypes.byref(p), ctypes.byref(b), budget)
-    rows = 8 * batch
-    pieces = max(1, min(-(-512 // rows), -(-budget // 16), 64))
-    slots = rows * pieces * 4 if pieces > 1 else 0
+    slots = 8 * batch * pieces * 4 if pieces > 1 else 0
     align = lambda x: (x + 255) & ~255  # noqa: E731
     assert size == align(align(2048 + slots * 8) + slots * 512)
 

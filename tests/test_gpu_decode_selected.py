@@ -148,7 +148,8 @@ def test_lists_of_several_windows(dtype, budget):
     _check(c, selected, counts, _decode(c, selected, counts), default_scale())
 
 
-@pytest.mark.parametrize("batch,hkv,budget", [(1, 1, 1000), (1, 8, 512), (3, 4, 200), (63, 8, 40), (64, 8, 40), (65, 8, 40)])
+@pytest.mark.parametrize("batch,hkv,budget", [(1, 1, 1000), (1, 8, 512), (3, 4, 200), (63, 8, 40), (64, 8, 40), (65, 8, 40),
+                                              (16, 8, 200), (32, 8, 130), (33, 8, 130), (48, 8, 129), (49, 8, 128)])
 def test_workgroups_to_a_list(batch, hkv, budget):
     c = _repeated(batch, 1024 if budget > 600 else 520, 2 * hkv, hkv, "bf16", seed=budget)
     selected, counts = _lists(c, budget, 1)

@@ -83,25 +83,28 @@ __device__ __forceinline__ double dot(u32x4 w, const double (&q)[C]) {
   return s;
 }
 
-// The sums of the loads U, U + 2^(B - B0), .. of w, dealt out to lane bits B0 (the last bit of a load's number) to TOP.
-template <typename T, bool F8, int TOP, int B, int U, int C>
-__device__ __forceinline__ double node(const u32x4* w, const double (&q)[C], int lane) {
-  if constexpr (B > TOP) return dot<T, F8>(w[U], q);
+// The sums d[U], d[U + 2^(B - B0)], .. dealt out to lane bits B0 (the last bit of a load's number) to TOP.
+template <int TOP, int B, int U>
+__device__ __forceinline__ double node(const double (&d)[8], int lane) {
+  if constexpr (B > TOP) return d[U];
   else {
-    const double a = node<T, F8, TOP, B + 1, U>(w, q, lane);
-    const double b = node<T, F8, TOP, B + 1, (U | 1 << (B - TOP + 2))>(w, q, lane);
+    const double a = node<TOP, B + 1, U>(d, lane);
+    const double b = node<TOP, B + 1, (U | 1 << (B - TOP + 2))>(d, lane);
     return halved<B>(a, b, lane);
   }
 }
 
-// The sums over a KV head's query heads of what is above and below zero, for each channel: [below | above].
+// The sums over a KV head's query heads of what is above and below zero, for each channel: [below | above], in runs of
+// C channels (a lane's) with two unused places behind each: lanes that read runs side by side meet no bank twice.
+template <int C>
 struct Query {
   double part[4][2 * kHeadDim];
+  double sum[2 * kHeadDim / C * (C + 2)];
 };
 // queries [group][128] of the KV head.  Every thread of the workgroup; ends with a barrier.  meanwhile() is called with the
 // loads on their way.
-template <typename T, typename F>
-__device__ __forceinline__ void sum_queries(const uint16_t* src, int group, Query& sm, F meanwhile) {
+template <typename T, int C, typename F>
+__device__ __forceinline__ void sum_queries(const uint16_t* src, int group, Query<C>& sm, F meanwhile) {
   const int c = threadIdx.x % kHeadDim, share = threadIdx.x / kHeadDim;   // heads share, share + 4, ..
   uint16_t w[4];
 #pragma unroll
@@ -118,7 +121,12 @@ __device__ __forceinline__ void sum_queries(const uint16_t* src, int group, Quer
   sm.part[share][c] = below;
   sm.part[share][kHeadDim + c] = above;
   __syncthreads();
+  const int i = threadIdx.x;
+  if (i < 2 * kHeadDim) sm.sum[i + i / C * 2] = (sm.part[0][i] + sm.part[1][i]) + (sm.part[2][i] + sm.part[3][i]);
+  __syncthreads();
 }
+
+constexpr int kOnce = 2;   // the non-temporal bit of the cache-policy operand
 
 // Scores of the blocks of a row of bounds.
 template <typename T, bool F8>
@@ -126,47 +134,49 @@ struct Scorer {
   static constexpr int kSpan = F8 ? 16 : 32, kTop = F8 ? 3 : 4, kChannels = F8 ? 16 : 8;   // lanes of a block; their number's last bit
   static constexpr int kTile = 8 * 64 / kSpan;                                             // blocks of 8 loads
   static constexpr int kRowBytes = F8 ? 2 * kHeadDim : 4 * kHeadDim;                       // of one block
-  const char* row;     // block 0
+  __amdgpu_buffer_rsrc_t row;   // n blocks
   int lane, n;
   double q[kChannels];
-  u32x4 w[2][8];
+  u32x4 w[8];
 
-  __device__ __forceinline__ void load(u32x4 (&to)[8], int t) const {   // a tile (blocks from n on: the last again)
-    const uint32_t at = (lane % kSpan) * 16;
+  // Load u of a tile; from block n on the descriptor's bound keeps it from memory.
+  __device__ __forceinline__ void load(int t, int u) {
+    const uint32_t at = (t + lane / kSpan * 8) * kRowBytes + (lane % kSpan) * 16;
+    w[u] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(row, at + u * kRowBytes, 0, kOnce));
+  }
+  __device__ __forceinline__ void load(int t) {
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      const uint32_t block = min(t + lane / kSpan * 8 + u, n - 1);
-      to[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(row + (block * kRowBytes + at)));
-    }
-    asm volatile("" ::: "memory");   // (else each load is moved to its use)
+    for (int u = 0; u < 8; ++u) load(t, u);
+    asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
   }
-  __device__ __forceinline__ void queries(const Query& sm) {
-    const int c0 = (lane % kSpan >= kSpan / 2 ? kHeadDim : 0) + kChannels * (lane % (kSpan / 2));   // (lower or upper bounds)
+  __device__ __forceinline__ void queries(const Query<kChannels>& sm) {
+    const double* run = sm.sum + lane % kSpan * (kChannels + 2);   // (lower bounds, then upper ones)
 #pragma unroll
-    for (int i = 0; i < kChannels; ++i) q[i] = (sm.part[0][c0 + i] + sm.part[1][c0 + i]) + (sm.part[2][c0 + i] + sm.part[3][c0 + i]);
+    for (int i = 0; i < kChannels; ++i) q[i] = run[i];
   }
-  // The score of block `of(t)` of the tile.
-  __device__ __forceinline__ double sum(const u32x4 (&from)[8]) const {
-    double x = node<T, F8, kTop, kTop - 2, 0>(from, q, lane);
-    if constexpr (!F8) x += moved<0x4E>(x);   // (lanes l ^ 2)
-    return x + moved<0xB1>(x);                // (lanes l ^ 1)
-  }
-  __device__ __forceinline__ int of(int t) const { return t + lane / kSpan * 8 + (lane >> (kTop - 2)) % 8; }
 
   // put(i, score of block i) for the blocks of tiles first, first + stride, .. below n, each by one lane; tile `first` is
-  // loaded already.  A tile's loads are in flight while the one before it is summed.
+  // loaded already.  Each load is followed by that of the next tile as soon as it is used: 8 in flight, from one copy
+  // of the code, which is fetched anew by each launch.
   template <typename F>
   __device__ __forceinline__ void scores(int first, int stride, F put) {
+    const int at = lane / kSpan * 8 + (lane >> (kTop - 2)) % 8;   // the lane's block of a tile
     const bool mine = lane % (1 << (kTop - 2)) == 0;
 #pragma unroll 1
-    for (int t = first; t < n; t += 2 * stride) {
-      load(w[1], t + stride);
-      const double a = sum(w[0]);
-      if (mine && of(t) < n) put(of(t), a);
-      load(w[0], t + 2 * stride);
-      const double b = sum(w[1]);
-      if (mine && of(t + stride) < n) put(of(t + stride), b);
+    for (int t = first; t < n; t += stride) {
+      double d[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        d[u] = dot<T, F8>(w[u], q);
+        load(t + stride, u);
+        asm volatile("" ::: "memory");   // (else each load is moved to its use)
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      double x = node<kTop, kTop - 2, 0>(d, lane);
+      if constexpr (!F8) x += moved<0x4E>(x);   // (lanes l ^ 2)
+      x += moved<0xB1>(x);                      // (lanes l ^ 1)
+      if (mine && t + at < n) put(t + at, x);
     }
   }
 };
@@ -406,7 +416,7 @@ __global__ __launch_bounds__(64 * kScanWaves, 4) void scan_kernel(SelectArgs a) 
   typedef Picker<kScanWaves, 1> P;
   extern __shared__ uint64_t keys[];   // [a.chunk]
   __shared__ typename P::Shared sm;
-  __shared__ Query query;
+  __shared__ Query<Scorer<T, F8>::kChannels> query;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row = blockIdx.x / (unsigned)a.chunks, part = blockIdx.x - row * a.chunks, s = row / (unsigned)a.num_kv_heads;
   const int n = blocks_of(a, s), c0 = part * a.chunk, need = a.budget - a.sink - a.recent;
@@ -420,10 +430,12 @@ __global__ __launch_bounds__(64 * kScanWaves, 4) void scan_kernel(SelectArgs a) 
   Scorer<T, F8> sc;
   sc.lane = lane;
   sc.n = c1 - c0;   // (offsets in a chunk fit 32 bits)
-  sc.row = static_cast<const char*>(a.bounds) + ((size_t)row * a.max_blocks + c0) * Scorer<T, F8>::kRowBytes;
+  sc.row = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<char*>(static_cast<const char*>(a.bounds)) + ((size_t)row * a.max_blocks + c0) * Scorer<T, F8>::kRowBytes, 0,
+      sc.n * Scorer<T, F8>::kRowBytes, 0x00020000);
   const int first = wave * Scorer<T, F8>::kTile;
   static_assert(kScanWaves * 64 == 4 * kHeadDim, "a thread a channel and share of the heads");
-  sum_queries<T>(a.q + (size_t)row * a.group * kHeadDim, a.group, query, [&]() { sc.load(sc.w[0], first); });
+  sum_queries<T>(a.q + (size_t)row * a.group * kHeadDim, a.group, query, [&]() { sc.load(first); });
   Range seen;
   if (first < sc.n) {
     sc.queries(query);

@@ -16,6 +16,7 @@
 // row is one chunk, that is the result.  Else the chunk's own best, as many as the budget could
 // take of it, go to the workspace, and join_kernel picks among those of all chunks the same way.
 #include <algorithm>
+#include <cstdint>
 
 #include "common.h"
 #include "long_context.h"
@@ -528,13 +529,32 @@ hipError_t run_typed(const SelectArgs& a, hipStream_t st) {
 
 }  // namespace
 
+// Chunks of 4096 (32 KiB of LDS) to 256 blocks.  A compute unit takes some 9 ns a block, 128 blocks' time more for a chunk's
+// queries and pick; a join costs 550 blocks' time and one for each 8 keys that the chunks keep.  (Not a
+// matter of `sink` and `recent`: a workspace serves all of them.)  us by chunk, the one that this takes in brackets:
+//   KV heads and blocks     4096     2048     1024      512      256
+//      256 x  2048                  [37.0]    42.9     42.7     49.2
+//      320 x  2048                   55.1     58.8    [51.9]    59.8
+//      152 x   880                           [17.4]    25.6     23.9
+//       72 x  6368, 8 bits   47.4    46.4    [33.4]    38.2     44.4
+//       64 x  8192, 8 bits   48.0   [32.9]    35.9     41.9     50.9
+//       24 x  8192           54.7    36.2    [29.9]    30.6     32.3
+//       32 x  2048                   26.3     22.7     18.4    [17.0]
+//        8 x 62501           64.4   [54.9]    64.7     76.0     96.5
 void plan_select(SelectArgs* a, int blocks) {
-  // Chunks of 512 to 4096 blocks (32 KiB of LDS), the largest that leave 240 workgroups of 8 waves
-  int chunk = 4096;
-  while (chunk > 512 && (int64_t)a->batch * a->num_kv_heads * ((blocks + chunk - 1) / chunk) < 240) chunk /= 2;
-  chunk = std::min(chunk, (blocks + 63) / 64 * 64);
-  a->chunk = std::max(chunk, 64);
-  a->chunks = std::max(1, (blocks + a->chunk - 1) / a->chunk);
+  constexpr int kUnits = 256;
+  const int64_t rows = (int64_t)a->batch * a->num_kv_heads;
+  int64_t least = INT64_MAX;
+  for (int most = 4096; most >= 256; most /= 2) {
+    const int chunk = std::max(64, std::min(most, (blocks + 63) / 64 * 64));
+    const int64_t chunks = std::max(1, (blocks + chunk - 1) / chunk);
+    int64_t cost = (rows * chunks + kUnits - 1) / kUnits * (chunk + 128);
+    if (chunks > 1) cost += 550 + chunks * std::min(chunk, a->budget) / 8;
+    if (cost >= least) continue;
+    least = cost;
+    a->chunk = chunk;
+    a->chunks = (int)chunks;
+  }
   a->kept = std::min(a->chunk, a->budget - a->sink - a->recent);
 }
 

@@ -94,6 +94,12 @@ def test_long_rows(dtype):
     r.check(12000, 4, 4)
 
 
+@pytest.mark.parametrize("sink,recent,budget", [(300, 0, 400), (0, 300, 400), (300, 299, 600), (300, 300, 600), (1, 2, 1199), (0, 0, 260)])
+def test_first_and_newest_blocks_over_parts_of_a_row(sink, recent, budget):
+    """Rows cut every few hundred blocks: parts that lie whole in the first or newest blocks, and shorter sequences."""
+    Rows([1200 * 16, 1199 * 16 - 5, 700 * 16, 257 * 16, 0], 8, 2, seed=budget).check(budget, sink, recent)
+
+
 def test_many_rows():
     rng = np.random.default_rng(4)
     Rows(rng.integers(0, 900, size=150), 8, 8, seed=4, max_blocks=70).check(16, 1, 1)

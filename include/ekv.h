@@ -837,8 +837,8 @@ ekv_status ekv_select_blocks(const ekv_pool* pool, const ekv_batch* batch, const
  *   counts    device int32 [batch][num_kv_heads], clamped into [0, budget]; NULL: budget
  *   ws        device scratch of ekv_decode_selected_workspace_bytes() bytes, 16-byte
  *             aligned, prepared by ekv_decode_workspace_init (or zero-filled) before
- *             its first use; it may be used with other batches; calls that share one
- *             must be ordered
+ *             its first use; it may be used with other batches and by ekv_attn_decode; calls
+ *             that share one must be ordered
  * A head without a token yields zeros.  q, out and the pool are 16-byte aligned.
  * Errors: as ekv_key_bounds; EKV_ERR_INVALID also for out_dtype, scale, budget and the
  * workspace; with EKV_DEBUG=1 for a block that is listed twice.

@@ -9,6 +9,7 @@
 #include "ekv.h"
 #include "host_checks.h"
 #include "host_status.h"
+#include "launch.h"
 #include "long_context.h"
 
 namespace {
@@ -16,7 +17,9 @@ namespace {
 using namespace ekv;
 
 constexpr int kMostRows = 1 << 22;   // (sequence, KV head)s of a call: grids stay within 2^32 threads
-constexpr int kCounters = 512;       // merge counters, at the start of a decode workspace whatever the batch
+// Counters at the start of a decode workspace, whatever the batch: as many as ekv_attn_decode keeps there, so that neither
+// call finds the other's partial results where it expects zeros.
+constexpr int kCounters = 2 * kMaxDecodeGrid;
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 

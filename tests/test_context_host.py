@@ -169,7 +169,7 @@ def test_decode_selected_workspace_sizes(lib, batch, budget, pieces):
     size = lib.ekv_decode_selected_workspace_bytes(ctypes.byref(p), ctypes.byref(b), budget)
     slots = 8 * batch * pieces * 4 if pieces > 1 else 0
     align = lambda x: (x + 255) & ~255  # noqa: E731
-    assert size == align(align(2048 + slots * 8) + slots * 512)
+    assert size == align(align(32768 + slots * 8) + slots * 512)
 
 
 def _device_batch():

@@ -224,7 +224,25 @@ def test_workspace_shared_by_batches_streams_and_repeats():
             assert np.array_equal(first.setdefault(id(x), out), out)   # the same sums every time
         side.wait_stream(torch.cuda.current_stream())
         assert np.array_equal(_decode(a, *lists[id(a)], ws=ws, stream=side), first[id(a)])
-    assert not ws[:2048].any()   # the counters are back at zero
+    assert not ws[:32768].any()   # the counters are back at zero
+
+
+def test_workspace_shared_with_the_dense_decode():
+    """In turn on one workspace, both with lists and sequences that are cut."""
+    torch = require_gpu()
+    c = Cache([4000, 900], 32, 8, seed=23, base=0.3)
+    n = c.bt.shape[1]
+    selected = np.broadcast_to(np.arange(n, dtype=np.int32), (2, 8, n)).copy()
+    sizes = ekv.decode_selected_workspace_bytes(c.kv.pool, c.batch, n), ekv.decode_workspace(c.kv.pool, c.batch).numel()
+    ws = torch.zeros(max(sizes), dtype=torch.uint8, device="cuda")
+    dense = torch.empty_like(c.q, dtype=torch.float32)
+    for _ in range(3):
+        out = _decode(c, selected, np.full((2, 8), n), ws=ws)
+        dense.fill_(7)
+        ekv.attn_decode(c.kv.pool, c.batch, c.q, dense, default_scale(), ws)
+        torch.cuda.synchronize()
+        _check(c, selected, np.full((2, 8), n), out, default_scale())
+        assert np.abs(out - dense.cpu().numpy()).max() <= 2e-5   # (as test_all_blocks_are_the_dense_decode)
 
 
 @pytest.mark.parametrize("batch", [2, 70])

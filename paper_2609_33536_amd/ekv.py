@@ -8,6 +8,7 @@ only); host mirrors as NumPy arrays.  A missing or unbuilt library raises
 """
 
 import ctypes
+import functools
 import os
 
 import numpy as np
@@ -518,6 +519,16 @@ def make_rope(turns, rotary_dim, layout="half", magnitude=1.0):
     return r
 
 
+@functools.lru_cache(maxsize=None)
+def _context_types(dtype):
+    """Torch's types around a pool of this dtype: of queries, of bounds, 32-bit integers, 32-bit floats.  (Looked up
+    once: a call's checks are half of what the smallest calls take.)"""
+    import torch
+    query = torch.bfloat16 if dtype == DTYPE_BF16 else torch.float16
+    kinds = (torch.float8_e5m2, torch.uint8) if dtype == DTYPE_E5M2 else (query, torch.int16)
+    return query, kinds, torch.int32, torch.float32
+
+
 def _rows(t, shape, dtype, name):
     """(pointer, row stride) of a tensor [n][heads][128] whose heads are packed."""
     if t.dtype is not dtype or t.shape != shape:
@@ -531,13 +542,13 @@ def _rows(t, shape, dtype, name):
 
 
 def _rope_arguments(pool, positions, slots, q, k, v, q_out):
-    import torch
+    dtype, _, int32, _ = _context_types(pool.dtype)
     n, hq, hkv = q.shape[0], q.shape[1], pool.num_kv_heads
-    dtype = torch.bfloat16 if pool.dtype == DTYPE_BF16 else torch.float16
-    (qp, qs), (op, os_) = _rows(q, (n, hq, HEAD_DIM), dtype, "q"), _rows(q_out, (n, hq, HEAD_DIM), dtype, "q_out")
-    (kp, ks), (vp, vs) = _rows(k, (n, hkv, HEAD_DIM), dtype, "k"), _rows(v, (n, hkv, HEAD_DIM), dtype, "v")
-    return (n, _typed(positions, torch.int32, (n,), "positions"), _typed(slots, torch.int32, (n,), "slots"), qp, qs, hq, kp,
-            ks, vp, vs, op, os_)
+    queries, keys = (n, hq, HEAD_DIM), (n, hkv, HEAD_DIM)
+    (qp, qs), (op, os_) = _rows(q, queries, dtype, "q"), _rows(q_out, queries, dtype, "q_out")
+    (kp, ks), (vp, vs) = _rows(k, keys, dtype, "k"), _rows(v, keys, dtype, "v")
+    return (n, _typed(positions, int32, (n,), "positions"), _typed(slots, int32, (n,), "slots"), qp, qs, hq, kp, ks, vp, vs, op,
+            os_)
 
 
 def rope_append(pool, rope, positions, slots, q, k, v, q_out, stream=None):
@@ -603,17 +614,8 @@ def attn_decode_shared(pool, prefixes, group_start, batch, q, out, scale, ws, st
                                         ws.numel() * ws.element_size(), _stream(stream)))
 
 
-def _query_type(pool):
-    import torch
-    return torch.bfloat16 if pool.dtype == DTYPE_BF16 else torch.float16
-
-
-def _bounds_ptr(pool, batch, bounds):
+def _bounds_ptr(bounds, kinds, shape):
     """Device pointer of bounds [batch][Hkv][max_blocks][2][128] of the pool's element type (or words of its size)."""
-    import torch
-    kinds = {DTYPE_BF16: (torch.bfloat16, torch.int16), DTYPE_FP16: (torch.float16, torch.int16),
-             DTYPE_E5M2: (torch.float8_e5m2, torch.uint8)}[pool.dtype]
-    shape = (batch.batch, pool.num_kv_heads, batch.max_blocks, 2, HEAD_DIM)
     if bounds is None or bounds.dtype not in kinds or bounds.shape != shape:
         raise EkvError(ERR_INVALID, f"bounds must be {kinds[0]} or {kinds[1]} {shape}")
     return _ptr(bounds)
@@ -629,9 +631,11 @@ def key_bounds_buffer(pool, batch, device="cuda"):
 def key_bounds(pool, batch, bounds, known=None, stream=None):
     """ekv_key_bounds: the smallest and largest keys of the blocks from
     known[s] / 16 on (int32 [batch]: tokens whose bounds are there; None: all)."""
-    import torch
-    _check(lib().ekv_key_bounds(ctypes.byref(pool), ctypes.byref(batch), _typed(known, torch.int32, (batch.batch,), "known"),
-                                _bounds_ptr(pool, batch, bounds), _stream(stream)))
+    _, kinds, int32, _ = _context_types(pool.dtype)
+    n = batch.batch
+    _check(lib().ekv_key_bounds(ctypes.byref(pool), ctypes.byref(batch), _typed(known, int32, (n,), "known"),
+                                _bounds_ptr(bounds, kinds, (n, pool.num_kv_heads, batch.max_blocks, 2, HEAD_DIM)),
+                                _stream(stream)))
 
 
 def _workspace(nbytes):
@@ -654,16 +658,15 @@ def select_blocks(pool, batch, q, bounds, selected, counts, ws, sink=1, recent=1
     """ekv_select_blocks: the blocks of the largest scores, into selected int32
     [batch][Hkv][budget] and counts int32 [batch][Hkv]; the first `sink` and the
     last `recent` blocks are always taken."""
-    import torch
-    rows = (batch.batch, pool.num_kv_heads)
     if selected is None or selected.dim() != 3:
         raise EkvError(ERR_INVALID, "selected must be int32 [batch][num_kv_heads][budget]")
-    budget = selected.shape[2]
+    dtype, kinds, int32, _ = _context_types(pool.dtype)
+    n, hkv, budget = batch.batch, pool.num_kv_heads, selected.shape[2]
     _check(lib().ekv_select_blocks(ctypes.byref(pool), ctypes.byref(batch),
-                                   _typed(q, _query_type(pool), (batch.batch, batch.num_q_heads, HEAD_DIM), "q"),
-                                   _bounds_ptr(pool, batch, bounds), budget, sink, recent,
-                                   _typed(selected, torch.int32, (*rows, budget), "selected"),
-                                   _typed(counts, torch.int32, rows, "counts"), _ptr(ws), ws.numel() * ws.element_size(),
+                                   _typed(q, dtype, (n, batch.num_q_heads, HEAD_DIM), "q"),
+                                   _bounds_ptr(bounds, kinds, (n, hkv, batch.max_blocks, 2, HEAD_DIM)), budget, sink, recent,
+                                   _typed(selected, int32, (n, hkv, budget), "selected"),
+                                   _typed(counts, int32, (n, hkv), "counts"), _ptr(ws), ws.numel() * ws.element_size(),
                                    _stream(stream)))
 
 
@@ -680,14 +683,14 @@ def decode_selected_workspace(pool, batch, budget, device="cuda"):
 def attn_decode_selected(pool, batch, selected, counts, q, out, scale, ws, stream=None):
     """Decode over the blocks selected int32 [batch][Hkv][budget], counts int32
     [batch][Hkv] of them (None: all; entries that are no block are passed over)."""
-    import torch
     if selected is None or selected.dim() != 3 or q is None or out is None:
         raise EkvError(ERR_INVALID, "selected [batch][num_kv_heads][budget], q and out are required")
-    rows, shape, dtype = (batch.batch, pool.num_kv_heads), (batch.batch, batch.num_q_heads, HEAD_DIM), _query_type(pool)
-    budget = selected.shape[2]
+    dtype, _, int32, float32 = _context_types(pool.dtype)
+    n, hkv, budget = batch.batch, pool.num_kv_heads, selected.shape[2]
+    shape, wide = (n, batch.num_q_heads, HEAD_DIM), out.dtype is float32
     _check(lib().ekv_attn_decode_selected(ctypes.byref(pool), ctypes.byref(batch),
-                                          _typed(selected, torch.int32, (*rows, budget), "selected"),
-                                          _typed(counts, torch.int32, rows, "counts"), budget, _typed(q, dtype, shape, "q"),
-                                          _typed(out, torch.float32 if out.dtype is torch.float32 else dtype, shape, "out"),
+                                          _typed(selected, int32, (n, hkv, budget), "selected"),
+                                          _typed(counts, int32, (n, hkv), "counts"), budget, _typed(q, dtype, shape, "q"),
+                                          _typed(out, float32 if wide else dtype, shape, "out"),
                                           dtype_code(out.dtype), scale, _ptr(ws), ws.numel() * ws.element_size(),
                                           _stream(stream)))

@@ -140,6 +140,7 @@ enum Norm { kNoNorm, kShared, kPerHead };
 // ONCE: inputs are read past the caches
 template <typename T, bool F8, bool ONCE, int NORM>
 __global__ __launch_bounds__(64 * kWaves) void rope_kernel(RopeArgs a) {
+  __shared__ float2 turns[kWaves][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 7;
   const int rows = a.num_q_heads + 2 * a.num_kv_heads;   // rows of a token: query heads, key heads, value heads
   const unsigned parts = (unsigned)(rows + a.rows_per_wave - 1) / a.rows_per_wave, item = blockIdx.x * kWaves + wave;
@@ -200,12 +201,17 @@ __global__ __launch_bounds__(64 * kWaves) void rope_kernel(RopeArgs a) {
   }
 
   const bool in_pool = slot >= 0 && slot / kPage < a.num_blocks;   // (outside the pool: the cache is left as it is)
+  // Lane i works pair i out, for the 8 lanes that hold it, one of each head.
+  float2 turn = make_float2(1.0f, 0.0f);
+  if (lane < 8 * turned) cos_sin((uint64_t)position * a.turns[lane], a.magnitude, turn.x, turn.y);
+  turns[wave][lane] = turn;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (of one wave: its LDS accesses stay in order)
+  __builtin_amdgcn_wave_barrier();
   float cs[8], sn[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    cs[i] = 1.0f;
-    sn[i] = 0.0f;
-    if (c < turned) cos_sin((uint64_t)position * a.turns[8 * c + i], a.magnitude, cs[i], sn[i]);
+    cs[i] = turns[wave][8 * c + i].x;
+    sn[i] = turns[wave][8 * c + i].y;
   }
 
   float qu[8], qv[8], ku[8], kv[8];

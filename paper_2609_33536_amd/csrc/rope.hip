@@ -249,21 +249,21 @@ __global__ __launch_bounds__(64 * kWaves) void rope_kernel(RopeArgs a) {
       }
       if (NORM != kNoNorm && c >= turned) {
         // (levelled, not turned)
-      } else if (a.pairs) {   // elements 16 c + 2 i, + 1
+      } else if (a.pairs) {   // elements 16 c + 2 i, + 1 (which product is fused is said, not left to the compiler)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float x0 = x[2 * i], x1 = x[2 * i + 1], y0 = y[2 * i], y1 = y[2 * i + 1];
-          x[2 * i] = x0 * cs[i] - x1 * sn[i];
-          x[2 * i + 1] = x1 * cs[i] + x0 * sn[i];
-          y[2 * i] = y0 * cs[4 + i] - y1 * sn[4 + i];
-          y[2 * i + 1] = y1 * cs[4 + i] + y0 * sn[4 + i];
+          x[2 * i] = fmaf(x0, cs[i], -(x1 * sn[i]));
+          x[2 * i + 1] = fmaf(x0, sn[i], x1 * cs[i]);
+          y[2 * i] = fmaf(y0, cs[4 + i], -(y1 * sn[4 + i]));
+          y[2 * i + 1] = fmaf(y0, sn[4 + i], y1 * cs[4 + i]);
         }
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const float x0 = x[i], y0 = y[i];
-          x[i] = x0 * cs[i] - y0 * sn[i];
-          y[i] = y0 * cs[i] + x0 * sn[i];
+          x[i] = fmaf(x0, cs[i], -(y0 * sn[i]));
+          y[i] = fmaf(y0, cs[i], x0 * sn[i]);
         }
       }
       w0 = words8<T>(x);

@@ -300,8 +300,8 @@ void launch_once(const RopeArgs& a, dim3 grid, dim3 block, bool once, hipStream_
 template <typename T, bool F8>
 void launch_typed(const RopeArgs& a, dim3 grid, dim3 block, bool once, hipStream_t st) {
   if (!a.norm) launch_once<T, F8, kNoNorm>(a, grid, block, once, st);
-  // (shared weights are worth keeping from 16 rows a wave on: 512 tokens of 32 / 8 heads 6.8 us, read a row 6.9, 2048 11.9 and
-  // 12.6; with 8 rows a wave, 64 tokens, 5.5 and 5.1)
+  // (shared weights are worth keeping from 16 rows a wave on: 1024 tokens of 32 / 8 heads 7.2 us, read a row 7.4, 2048 9.5 and
+  // 9.9, 8192 36.4 and 37.8; with 8 rows a wave, 512 tokens, 5.1 and 4.8)
   else if (a.q_weight_stride == 0 && a.k_weight_stride == 0 && a.rows_per_wave > 8) launch_once<T, F8, kShared>(a, grid, block, once, st);
   else launch_once<T, F8, kPerHead>(a, grid, block, once, st);
 }
@@ -312,13 +312,13 @@ hipError_t launch_rope(const RopeArgs& a, int dtype, hipStream_t st) {
   if (a.n == 0) return hipSuccess;
   RopeArgs b = a;
   const int rows = a.num_q_heads + 2 * a.num_kv_heads;
-  // A wave works the angles out once for its rows, 8 at a time: as many rows as leave 2048
-  // waves (8 a CU).  Measured with 48 rows a token, us at 8 / 16 / 24 / 48 rows a wave:
-  // 64 tokens 4.4 / 4.8 / 5.3 / 6.7, 512 tokens 6.1 / 5.7 / 6.1 / 7.4, 1024 tokens
-  // 9.2 / 7.5 / 7.0 / 7.9, 8192 tokens 52.1 / 41.2 / 38.5 / 37.6.
-  const int64_t share = ((int64_t)a.n * rows + 2047) / 2048;
+  // A wave works the angles out once for its rows, 8 at a time: as many rows as leave 4096
+  // waves (16 a CU).  Measured with 48 rows a token, us at 1024 / 2048 / 4096 / 8192 waves:
+  // 64 tokens 2.9 at any (8 rows a wave), 512 tokens 4.6 / 4.3 / 4.0 / 3.9, 1024 tokens
+  // 7.0 / 6.4 / 6.1 / 6.3, 2048 9.7 / 9.7 / 9.0 / 9.1, 8192 36.1 / 35.7 / 35.6 / 35.5.
+  const int64_t share = ((int64_t)a.n * rows + 4095) / 4096;
   b.rows_per_wave = (int)std::min<int64_t>((share + 7) / 8 * 8, rows);
-  const int64_t waves = (int64_t)a.n * ((rows + b.rows_per_wave - 1) / b.rows_per_wave);   // (at most 2048 + a.n)
+  const int64_t waves = (int64_t)a.n * ((rows + b.rows_per_wave - 1) / b.rows_per_wave);   // (at most 4096 + a.n)
   // Inputs of 32 MB and more are read past the caches, which the outputs, read next, then
   // have to themselves: a copy that makes q, k and v, this kernel and a copy of its queries
   // take 105.5 us for 8192 tokens of 48 rows (111.3 with plain loads), 58.5 (59.9) for

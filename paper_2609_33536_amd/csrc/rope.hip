@@ -12,14 +12,16 @@
 // elements 8c.. and rotary_dim / 2 + 8c..; pair layout: 16c .. 16c + 15), so that a
 // lane's cosines and sines serve every head that its wave turns.  The kernel is bound
 // by HBM: q in and out, k and v in, their cache rows out.  16384 tokens of 64 + 2 x 8 heads
-// into an 8-bit pool, not in a cache, take 128 us (638 MB, 5.0 TB/s; a plain copy reaches
-// 5.2), 64 tokens of 32 + 2 x 8 heads 4.4 us (a launch).
+// into an 8-bit pool, not in a cache, take 126 us (638 MB, 5.0 TB/s; a plain copy reaches
+// 5.2), 64 tokens of 32 + 2 x 8 heads 3.4 us (a launch).  A wave's lane works out one pair's angle
+// and passes it on through LDS (each of a head's 8 lanes for itself, all of them eight times over: 128 and 4.4 us,
+// 2048 tokens with norms 11.9 where they are 9.6 now).
 //
 // Heads may be levelled first (the norms of queries and keys): x / sqrt(mean(x^2) + eps) (offset +
 // weight) in the same registers, the squares summed over the 8 lanes, so that a norm adds no byte but
-// its weights.  16384 tokens of 64 + 2 x 8 heads into an 8-bit pool take 129 us with norms as without;
-// 8192 of 32 + 2 x 8 into a 16-bit one 43 (38.5 without: its vector work, 350 instructions a
-// wave and 8 rows, is as long as its loads and stores and not all hidden), 64 5.1.
+// its weights.  16384 tokens of 64 + 2 x 8 heads into an 8-bit pool take 126 us with norms as without;
+// 8192 of 32 + 2 x 8 into a 16-bit one 38.1 (35.6 without: its vector work, 350 instructions a
+// wave and 8 rows, is not all hidden behind its loads and stores), 64 4.0.
 #include <algorithm>
 
 #include "common.h"
@@ -38,7 +40,7 @@ constexpr int kWaves = 4;
 // rounds away carried through the product with m.  Products are fused where it says so
 // and nowhere else: one that is added fused and subtracted rounded would count what it
 // rounds away twice (that, and m on a rounded sum, left 16 to 42 % more 16-bit outputs
-// that are not the nearest; 64 tokens 4.3 us then, 4.4 now).
+// that are not the nearest; 64 tokens 4.3 us then, 4.4 with it).
 __device__ __forceinline__ void cos_sin(uint64_t p, float m, float& c, float& s) {
 #pragma clang fp contract(off)
   constexpr double kUnit = 1.46291807926715968e-9;   // 2 pi / 2^32

@@ -88,13 +88,12 @@ SelectArgs select_args(const ekv_pool* pool, const ekv_batch* b, int group, int3
 // Scratch of a decode over selected blocks: [merge counters | (m, l) | o], 256-B aligned parts
 struct SelectedLayout {
   size_t ml, o, total;
-  int pieces;
 };
 SelectedLayout selected_layout(const ekv_pool* pool, const ekv_batch* b, int32_t budget, int group) {
   SelectedLayout l{};
   const int64_t rows = (int64_t)b->batch * pool->num_kv_heads;
-  l.pieces = selected_pieces(rows, budget);
-  const size_t slots = l.pieces > 1 ? (size_t)rows * l.pieces * group : 0;
+  const int pieces = selected_pieces(rows, budget);   // (no fewer for a larger budget)
+  const size_t slots = pieces > 1 ? (size_t)rows * pieces * group : 0;
   l.ml = align256(kCounters * sizeof(uint32_t));
   l.o = align256(l.ml + slots * 2 * sizeof(float));
   l.total = align256(l.o + slots * kHeadDim * sizeof(float));
@@ -229,7 +228,8 @@ ekv_status ekv_attn_decode_selected(const ekv_pool* pool, const ekv_batch* batch
     a.out = out;
     a.num_q_heads = batch->num_q_heads;
     a.budget = budget;
-    a.pieces = l.pieces;
+    // (no list needs more than its sequence's blocks; the workspace's size is that of the budget whatever the lengths)
+    a.pieces = selected_pieces((int64_t)batch->batch * pool->num_kv_heads, std::min(budget, max_seq_blocks(batch)));
     a.out_fp32 = out_dtype == EKV_DTYPE_FP32;
     a.scale_log2 = log2e_scale(scale);
     return hip_status(launch_selected(a, pool->dtype, group, batch->mode != EKV_MODE_NATIVE, stream),

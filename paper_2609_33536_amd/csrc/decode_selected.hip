@@ -495,11 +495,11 @@ hipError_t run_group(const SelectedArgs& a, int group, bool elastic, hipStream_t
 // Lists of up to 32 blocks take less uncut (9.1, in two pieces 9.6).  A little above 256 lists some compute units
 // have two workgroups and most one: lists of 128 blocks or more are halved up to 384 of them (33 sequences
 // 103.6 -> 87.4, 8-bit 56.5 -> 53.3; 48: 109.6 -> 102.7, 62.6 -> 60.7; but 56: 114.9 -> 124.8, 67.2 -> 76.2).
-int selected_pieces(int64_t rows, int budget) {
+int selected_pieces(int64_t rows, int blocks) {
   constexpr int kUnits = 256;
-  if (budget <= 32 || rows <= 0) return 1;
-  if (rows > kUnits) return rows <= kUnits * 3 / 2 && budget >= 128 ? 2 : 1;
-  return (int)std::min<int64_t>({kUnits / rows, (budget + 4 * kTeam - 1) / (4 * kTeam), kMostPieces});
+  if (blocks <= 32 || rows <= 0) return 1;
+  if (rows > kUnits) return rows <= kUnits * 3 / 2 && blocks >= 128 ? 2 : 1;
+  return (int)std::min<int64_t>({kUnits / rows, (blocks + 4 * kTeam - 1) / (4 * kTeam), kMostPieces});
 }
 
 hipError_t launch_selected(const SelectedArgs& a, int dtype, int group, bool elastic, hipStream_t st) {

@@ -56,8 +56,8 @@ struct SelectedArgs {
   int32_t num_q_heads, budget, pieces, out_fp32;
   float scale_log2;          // softmax scale * log2(e)
 };
-// Workgroups that share a (sequence, KV head)'s list.
-int selected_pieces(int64_t rows, int budget);
+// Workgroups that share the list of a (sequence, KV head), of up to `blocks` blocks.
+int selected_pieces(int64_t rows, int blocks);
 hipError_t launch_selected(const SelectedArgs& a, int dtype, int group, bool elastic, hipStream_t st);
 
 }  // namespace ekv

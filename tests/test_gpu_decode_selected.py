@@ -156,6 +156,18 @@ def test_workgroups_to_a_list(batch, hkv, budget):
     _check(c, selected, counts, _decode(c, selected, counts), default_scale())
 
 
+@pytest.mark.parametrize("lengths", [[1, 2, 3], [40, 17, 0], [500, 512, 1]])
+@pytest.mark.parametrize("batch,budget", [(1, 700), (13, 165), (3, 33)])
+def test_budgets_beyond_the_sequences(lengths, batch, budget):
+    """Fewer blocks than the budget has room for, with strays behind them: workgroups go by the blocks."""
+    c = Cache(lengths * batch, 16, 8, seed=budget)
+    n = -(-max(lengths) // 16)
+    selected = np.full((3 * batch, 8, budget), -1, dtype=np.int32)
+    selected[:, :, :n] = np.arange(n)
+    counts = np.full((3 * batch, 8), budget)
+    _check(c, selected, counts, _decode(c, selected, counts), default_scale())
+
+
 def test_all_blocks_are_the_dense_decode():
     torch = require_gpu()
     c = Cache([500, 77, 0, 1029], 32, 8, base=0.4, seed=16)

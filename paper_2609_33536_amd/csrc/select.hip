@@ -21,19 +21,12 @@
 #include <cstdint>
 
 #include "common.h"
+#include "key_bins.h"
 #include "long_context.h"
 #include "wave_scan.h"
 
 namespace ekv {
 namespace {
-
-// A score as an integer that orders as it does, above 1; what is not a number above all scores.
-constexpr uint64_t kNotNumber = ~0ull;
-__device__ __forceinline__ uint64_t score_key(double x) {
-  if (x != x) return kNotNumber;
-  const uint64_t w = __builtin_bit_cast(uint64_t, x + 0.0);   // (-0 is 0)
-  return w >> 63 ? ~w : w | 1ull << 63;
-}
 
 template <int CTRL>
 __device__ __forceinline__ double moved(double x) {
@@ -291,16 +284,16 @@ struct Picker {
     all.from = sm.low[lane % (4 * WAVES)];
     all.to = sm.high[lane % (4 * WAVES)];
     all.over_row();
-    uint64_t from = ~0ull, to = 0;
+    KeyBins in{~0ull, 0};   // the last key lies here, `need` of these from the top; a pass divides the range by 512 or more
 #pragma unroll
     for (int r = 0; r < WAVES / 4; ++r) {
-      from = lower(from, lane_key(all.from, 16 * r));
-      to = higher(to, lane_key(all.to, 16 * r));
+      in.from = lower(in.from, lane_key(all.from, 16 * r));
+      in.to = higher(in.to, lane_key(all.to, 16 * r));
     }
-    while (from < to) {   // the last key lies in [from, to], `need` of those from the top; a pass divides the range by 512 or more
-      const int shift = max(0, 54 - __builtin_clzll(to - from));   // (to - from) >> shift < 1024
+    while (in.from < in.to) {
+      const int shift = in.shift();
       each_key(keys, lo, hi, [&](uint64_t k) {
-        if (k >= from && k <= to) atomicAdd(&sm.bins[(k - from) >> shift], 1u);
+        if (in.holds(k)) atomicAdd(&sm.bins[in.bin(k, shift)], 1u);
       });
       __syncthreads();
       if (wave == 0) {   // bins from the top, 16 a lane: the one in which the count reaches `need`
@@ -320,16 +313,15 @@ struct Picker {
       __syncthreads();
       const int bin = __builtin_amdgcn_readfirstlane(sm.bin), count = __builtin_amdgcn_readfirstlane(sm.bins[bin]);
       need -= __builtin_amdgcn_readfirstlane(sm.over);
-      from += (uint64_t)bin << shift;
-      to = lower(to, from + ((1ull << shift) - 1));
+      in.enter(bin, shift);
       if (need == count) {   // all of the bin (no key is 0 or 1: none is taken for the one below it)
-        --from;
+        --in.from;
         need = 0;
         break;
       }
-      if (count <= kRanked && from < to) {   // few: ranked among themselves
+      if (count <= kRanked && in.from < in.to) {   // few: ranked among themselves
         each_key(keys, lo, hi, [&](uint64_t k) {
-          if (k >= from && k <= to) sm.list[atomicAdd(&sm.listed, 1) % kRanked] = k;
+          if (in.holds(k)) sm.list[atomicAdd(&sm.listed, 1) % kRanked] = k;
         });
         __syncthreads();
         if (wave == 0) rank(lane < count ? sm.list[lane] : 0, count, need, sm);
@@ -341,7 +333,7 @@ struct Picker {
       __syncthreads();
     }
     if (threadIdx.x == 0) {
-      sm.last = from;
+      sm.last = in.from;
       sm.ties = need;
     }
     __syncthreads();
@@ -460,10 +452,13 @@ __global__ __launch_bounds__(64 * kScanWaves, 4) void scan_kernel(SelectArgs a) 
   }
   if (a.chunks == 1) {
     int32_t* out = a.selected + (size_t)row * a.budget + a.sink;
-    P::list_above(keys, lo, hi, last, ties, sm, [&](int place, int i) { out[place] = i; });
+    P::list_above(keys, lo, hi, last, ties, sm, [&](int place, int i) {
+      if (place < need) out[place] = i;   // (never more: the list's end does not hang on the pick)
+    });
   } else {
     const size_t at = ((size_t)row * a.chunks + part) * a.kept;
     P::list_above(keys, lo, max(lo, hi), last, ties, sm, [&](int place, int i) {
+      if (place >= a.kept) return;   // (nor the chunk's)
       a.keys[at + place] = keys[i];
       a.blocks[at + place] = c0 + i;
     });

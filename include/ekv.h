@@ -805,7 +805,8 @@ ekv_status ekv_key_bounds(const ekv_pool* pool, const ekv_batch* batch, const in
  * which no key of the block exceeds in sum_g q_g . k.  It is computed in 64 bits.  Of
  * the n blocks that hold tokens, the first `sink` and the last `recent` are taken, and of the others
  * those with the largest scores (the lowest block first among equals; a score that is
- * not a number is the largest), min(n, budget) in all.  (A negative softmax scale turns
+ * not a number is the largest, above infinity, and every score of a KV head is one with
+ * a query that is not a number), min(n, budget) in all.  (A negative softmax scale turns
  * the order of scores round; it is not known here.)
  *   q         device [batch][num_q_heads][head_dim], query dtype (the pool's, or FP16
  *             for an 8-bit pool)

@@ -111,8 +111,8 @@ __device__ __forceinline__ void sum_queries(const uint16_t* src, int group, Quer
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     const float x = share + 4 * k < group ? Mma<T>::widen(w[k]) : 0.f;
-    below += (double)(x < 0.f ? x : 0.f);   // (a NaN counts as nothing)
-    above += (double)(x > 0.f ? x : 0.f);
+    below += (double)(x > 0.f ? 0.f : x);   // (a NaN is on both sides: no score of the KV head is a number then)
+    above += (double)(x < 0.f ? 0.f : x);
   }
   sm.part[share][c] = below;
   sm.part[share][kHeadDim + c] = above;

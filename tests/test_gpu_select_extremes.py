@@ -71,3 +71,20 @@ def test_what_is_no_number_comes_before_infinity_and_that_by_block(budget, want)
     q[0, :, 5], q[0, :, 6] = 1.0, [0.5, -0.5]
     r = Rows([16 * n], 2, 1, bounds=workloads.to_words(v, "bf16"), q=workloads.to_words(q, "bf16"))
     assert r.select(budget, 0, 0)[0][0, 0].tolist() == want
+
+
+@pytest.mark.parametrize("lens", [[2000, 700, 333], [19200, 700, 16000]])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "e5m2"])
+@pytest.mark.parametrize("group,head,sign", [(1, 0, 0), (4, 3, 1), (16, 9, 0)])
+def test_queries_that_are_no_numbers(lens, dtype, group, head, sign):
+    """Every score of their KV head is undefined then: the first blocks among equals.  Other heads and sequences keep
+    their lists."""
+    half = workloads.query_dtype(dtype)
+    q = workloads.to_words(np.random.default_rng(group).standard_normal((3, 2 * group, 128), dtype=np.float32), half)
+    q[1, head, 77] = (0x7FC0 if half == "bf16" else 0x7E00) | sign << 15
+    r = Rows(lens, 2 * group, 2, dtype, seed=group, q=q)
+    r.check(20, 1, 2)
+    r.check(30, 0, 0)
+    got, _ = r.select(20, 1, 2)
+    n = -(-lens[1] // 16)
+    assert got[1, 0].tolist() == [*range(18), n - 2, n - 1]

@@ -13,7 +13,7 @@ their definitions:
   beyond the infinity of its sign.
 * ``select``  -- a block's score is the sum over channels of the larger of q lo and
   q hi, over the query heads of a KV head; first and newest blocks, then the largest
-  scores, the lowest block first among equals.
+  scores, what is no number above infinity, the lowest block first among equals.
 * ``decode``  -- softmax attention over the tokens of the listed blocks.
 """
 
@@ -77,9 +77,10 @@ def select(q, bounds_words, seq_lens, budget, sink, recent, dtype):
         for h in range(hkv):
             x = values(bounds_words[s, h, :n], dtype)
             rank = scores(q[s, h * group:(h + 1) * group], x[:, 0], x[:, 1])
-            rank[np.isnan(rank)] = np.inf
+            undefined = np.isnan(rank)   # (above infinity)
+            rank[undefined] = np.inf
             ends = [i for i in range(n) if i < sink or i >= n - recent]
-            middle = sorted(range(min(sink, n), max(min(sink, n), n - recent)), key=lambda i: (-rank[i], i))
+            middle = sorted(range(min(sink, n), max(min(sink, n), n - recent)), key=lambda i: (not undefined[i], -rank[i], i))
             chosen = sorted((ends + middle)[:budget])
             selected[s, h, :len(chosen)] = chosen
             counts[s, h] = len(chosen)

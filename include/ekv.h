@@ -814,8 +814,9 @@ ekv_status ekv_key_bounds(const ekv_pool* pool, const ekv_batch* batch, const in
  *   selected  device int32 [batch][num_kv_heads][budget]: the logical blocks in
  *             ascending order, then -1
  *   counts    device int32 [batch][num_kv_heads]: min(n, budget)
- *   ws        device scratch of ekv_select_workspace_bytes() bytes (of one size for
- *             all sink and recent), 16-byte aligned; needs no preparation and keeps
+ *   ws        device scratch of ekv_select_workspace_bytes() bytes, 16-byte aligned; one
+ *             that is made for the largest batch, length and budget serves every smaller
+ *             call, and all sink and recent; needs no preparation and keeps
  *             nothing between calls; calls that share one must be ordered
  * 0 <= sink, recent; sink + recent <= budget < 2^20.  Of the pool only its shape and of the
  * batch its lengths and sizes are used.

@@ -57,13 +57,11 @@ ekv_status check_budget(int32_t budget) {
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Scratch of a selection whose rows take several chunks: [keys u64 | block numbers], 256-B aligned parts.
-// (The chunks keep the most with no first and newest blocks.)
+// Scratch of a selection whose rows take several chunks: [keys u64 | block numbers], 256-B aligned parts, for `kept` of both.
 struct SelectLayout {
   size_t blocks, total;
 };
-SelectLayout select_layout(const SelectArgs& a) {
-  const size_t kept = a.chunks > 1 ? (size_t)a.batch * a.num_kv_heads * a.chunks * a.kept : 0;
+SelectLayout select_layout(size_t kept) {
   SelectLayout l{};
   l.blocks = align256(kept * sizeof(uint64_t));
   l.total = std::max<size_t>(256, l.blocks + align256(kept * sizeof(int32_t)));
@@ -153,7 +151,7 @@ ekv_status ekv_key_bounds(const ekv_pool* pool, const ekv_batch* batch, const in
 size_t ekv_select_workspace_bytes(const ekv_pool* pool, const ekv_batch* batch, int32_t budget) {
   int group = 0;
   if (check_rows(pool, batch, &group) != EKV_OK || check_budget(budget) != EKV_OK) return 0;
-  return select_layout(select_args(pool, batch, group, budget, 0, 0)).total;
+  return select_layout((size_t)batch->batch * pool->num_kv_heads * most_kept(max_seq_blocks(batch), budget)).total;
 }
 
 ekv_status ekv_select_blocks(const ekv_pool* pool, const ekv_batch* batch, const void* q, const void* bounds, int32_t budget,
@@ -171,7 +169,7 @@ ekv_status ekv_select_blocks(const ekv_pool* pool, const ekv_batch* batch, const
     if (batch->batch == 0) return EKV_OK;
     if (!q || !bounds || !selected || !counts) return fail(EKV_ERR_INVALID, "q, bounds, selected and counts are required");
     SelectArgs a = select_args(pool, batch, group, budget, sink, recent);
-    const SelectLayout l = select_layout(a);
+    const SelectLayout l = select_layout(a.chunks > 1 ? (size_t)a.batch * a.num_kv_heads * a.chunks * a.kept : 0);
     const size_t need = l.total;
     if (!ws || ws_bytes < need)
       return fail(EKV_ERR_INVALID, "workspace of %zu bytes needed, %zu given", need, ws ? ws_bytes : (size_t)0);

@@ -42,6 +42,9 @@ struct SelectArgs {
 };
 // Fills in the chunks for rows of at most `blocks` blocks.
 void plan_select(SelectArgs* a, int blocks);
+// The most that chunks * kept of a plan with several chunks can be, for any number of rows of at most `blocks` blocks and
+// any budget up to this one: it grows with both.
+size_t most_kept(int blocks, int budget);
 hipError_t launch_select(const SelectArgs& a, int dtype, hipStream_t st);
 
 struct SelectedArgs {

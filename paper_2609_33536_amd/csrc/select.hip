@@ -541,11 +541,12 @@ hipError_t run_typed(const SelectArgs& a, hipStream_t st) {
 //       24 x  8192           54.7    36.2    [29.9]    30.6     32.3
 //       32 x  2048                   26.3     22.7     18.4    [17.0]
 //        8 x 62501           64.4   [54.9]    64.7     76.0     96.5
+constexpr int kMostChunk = 4096, kLeastChunk = 256;
 void plan_select(SelectArgs* a, int blocks) {
   constexpr int kUnits = 256;
   const int64_t rows = (int64_t)a->batch * a->num_kv_heads;
   int64_t least = INT64_MAX;
-  for (int most = 4096; most >= 256; most /= 2) {
+  for (int most = kMostChunk; most >= kLeastChunk; most /= 2) {
     const int chunk = std::max(64, std::min(most, (blocks + 63) / 64 * 64));
     const int64_t chunks = std::max(1, (blocks + chunk - 1) / chunk);
     int64_t cost = (rows * chunks + kUnits - 1) / kUnits * (chunk + 128);
@@ -556,6 +557,15 @@ void plan_select(SelectArgs* a, int blocks) {
     a->chunks = (int)chunks;
   }
   a->kept = std::min(a->chunk, a->budget - a->sink - a->recent);
+}
+
+// (Of every chunk that the loop above may take, whichever it takes: fewer rows may need more of it than many, and a workspace
+// for the most serves all.  A row keeps less than a chunk more than its blocks, 12 bytes each, where their bounds have 512 or 256.)
+size_t most_kept(int blocks, int budget) {
+  size_t most = 0;
+  for (int chunk = kMostChunk; chunk >= kLeastChunk; chunk /= 2)
+    if (blocks > chunk) most = std::max(most, (size_t)((blocks + chunk - 1) / chunk) * std::min(chunk, budget));
+  return most;
 }
 
 hipError_t launch_select(const SelectArgs& a, int dtype, hipStream_t st) {

@@ -840,7 +840,10 @@ ekv_status ekv_select_blocks(const ekv_pool* pool, const ekv_batch* batch, const
  *   ws        device scratch of ekv_decode_selected_workspace_bytes() bytes, 16-byte
  *             aligned, prepared by ekv_decode_workspace_init (or zero-filled) before
  *             its first use; it may be used with other batches and by ekv_attn_decode; calls
- *             that share one must be ordered
+ *             that share one must be ordered.  Few lists are cut into pieces and need more
+ *             than many that are not: a workspace for a batch that changes has the largest of
+ *             its sizes.  Every size that the function reports is taken for every batch,
+ *             though: lists are then cut into as many pieces as it has room for
  * A head without a token yields zeros.  q, out and the pool are 16-byte aligned.
  * Errors: as ekv_key_bounds; EKV_ERR_INVALID also for out_dtype, scale, budget and the
  * workspace; with EKV_DEBUG=1 for a block that is listed twice.

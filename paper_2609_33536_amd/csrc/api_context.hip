@@ -83,14 +83,14 @@ SelectArgs select_args(const ekv_pool* pool, const ekv_batch* b, int group, int3
   return a;
 }
 
-// Scratch of a decode over selected blocks: [merge counters | (m, l) | o], 256-B aligned parts
+// Scratch of a decode over selected blocks whose lists are cut into `pieces`: [merge counters | (m, l) | o], 256-B aligned
+// parts.  The size does not grow with the batch (many lists are not cut), so a call takes any workspace that holds the
+// counters and cuts its lists into no more pieces than there is room for.
 struct SelectedLayout {
   size_t ml, o, total;
 };
-SelectedLayout selected_layout(const ekv_pool* pool, const ekv_batch* b, int32_t budget, int group) {
+SelectedLayout selected_layout(int64_t rows, int pieces, int group) {
   SelectedLayout l{};
-  const int64_t rows = (int64_t)b->batch * pool->num_kv_heads;
-  const int pieces = selected_pieces(rows, budget);   // (no fewer for a larger budget)
   const size_t slots = pieces > 1 ? (size_t)rows * pieces * group : 0;
   l.ml = align256(kCounters * sizeof(uint32_t));
   l.o = align256(l.ml + slots * 2 * sizeof(float));
@@ -189,7 +189,8 @@ ekv_status ekv_select_blocks(const ekv_pool* pool, const ekv_batch* batch, const
 size_t ekv_decode_selected_workspace_bytes(const ekv_pool* pool, const ekv_batch* batch, int32_t budget) {
   int group = 0;
   if (check_rows(pool, batch, &group) != EKV_OK || check_budget(budget) != EKV_OK) return 0;
-  return selected_layout(pool, batch, budget, group).total;
+  const int64_t rows = (int64_t)batch->batch * pool->num_kv_heads;
+  return selected_layout(rows, selected_pieces(rows, budget), group).total;   // (no fewer pieces for a larger budget)
 }
 
 ekv_status ekv_attn_decode_selected(const ekv_pool* pool, const ekv_batch* batch, const int32_t* selected,
@@ -206,7 +207,11 @@ ekv_status ekv_attn_decode_selected(const ekv_pool* pool, const ekv_batch* batch
     if (out_dtype != q_dtype && out_dtype != EKV_DTYPE_FP32)
       return fail(EKV_ERR_INVALID, "out_dtype must be the query dtype or fp32");
     if (!std::isfinite(scale)) return fail(EKV_ERR_INVALID, "scale must be finite");
-    const SelectedLayout l = selected_layout(pool, batch, budget, group);
+    const int64_t rows = (int64_t)batch->batch * pool->num_kv_heads;
+    // (no list needs more than its sequence's blocks; the reported size is that of the budget whatever the lengths)
+    int pieces = selected_pieces(rows, std::min(budget, max_seq_blocks(batch)));
+    SelectedLayout l = selected_layout(rows, pieces, group);
+    while (pieces > 1 && l.total > ws_bytes) l = selected_layout(rows, --pieces, group);
     if (!ws || ws_bytes < l.total)
       return fail(EKV_ERR_INVALID, "workspace of %zu bytes needed, %zu given", l.total, ws ? ws_bytes : (size_t)0);
     if (!aligned16(ws) || !aligned16(q) || !aligned16(out) || !aligned16(pool->kv))
@@ -226,8 +231,7 @@ ekv_status ekv_attn_decode_selected(const ekv_pool* pool, const ekv_batch* batch
     a.out = out;
     a.num_q_heads = batch->num_q_heads;
     a.budget = budget;
-    // (no list needs more than its sequence's blocks; the workspace's size is that of the budget whatever the lengths)
-    a.pieces = selected_pieces((int64_t)batch->batch * pool->num_kv_heads, std::min(budget, max_seq_blocks(batch)));
+    a.pieces = pieces;
     a.out_fp32 = out_dtype == EKV_DTYPE_FP32;
     a.scale_log2 = log2e_scale(scale);
     return hip_status(launch_selected(a, pool->dtype, group, batch->mode != EKV_MODE_NATIVE, stream),

@@ -675,9 +675,14 @@ def decode_selected_workspace_bytes(pool, batch, budget):
 
 
 def decode_selected_workspace(pool, batch, budget, device="cuda"):
-    """A zero-filled workspace for :func:`attn_decode_selected` (its merge counters start at zero)."""
+    """A zero-filled workspace for :func:`attn_decode_selected` (its merge counters start at zero), of the size that this
+    batch and every smaller one need at most: few lists are cut into pieces, many are not."""
     import torch
-    return torch.zeros(_workspace(decode_selected_workspace_bytes(pool, batch, budget)), dtype=torch.uint8, device=device)
+    size = _workspace(decode_selected_workspace_bytes(pool, batch, budget))
+    part = Batch.from_buffer_copy(batch)
+    for part.batch in range(1, min(batch.batch, 1 + 512 // pool.num_kv_heads)):   # (more lists are not cut)
+        size = max(size, decode_selected_workspace_bytes(pool, part, budget))
+    return torch.zeros(size, dtype=torch.uint8, device=device)
 
 
 def attn_decode_selected(pool, batch, selected, counts, q, out, scale, ws, stream=None):

@@ -7,7 +7,7 @@ import itertools
 import pytest
 
 from paper_2609_33536_amd import ekv
-from tests.test_context_host import SELECT, lib  # noqa: F401
+from tests.test_context_host import SELECT, SELECTED, lib  # noqa: F401
 from tests.test_serve_host import AT, INVALID, _batch, _pool, _refused
 
 BATCHES = [*range(1, 70), 96, 128, 200, 333, 512]
@@ -59,3 +59,32 @@ def test_a_selection_workspace_serves_every_smaller_call(lib, batch, blocks, bud
         bt = _batch(batch=b, max_blocks=blocks, max_seq_len=16 * n)
         a = dict(SELECT, budget=k, sink=sink, recent=0, q=AT + 4, ws_bytes=size)   # (refused behind the workspace's check)
         _refused(lib, lib.ekv_select_blocks(ctypes.byref(pool), ctypes.byref(bt), *a.values(), None), INVALID, "aligned")
+
+
+@pytest.mark.parametrize("hkv,group", [(8, 4), (1, 16), (8, 16)])
+def test_every_reported_decode_workspace_is_taken_for_every_batch(lib, hkv, group):  # noqa: F811
+    pool = _pool(num_kv_heads=hkv)
+    sizes = {}
+    for b, k in itertools.product(BATCHES, (1, 33, 128, 256, 1000)):
+        bt = _batch(batch=b, max_blocks=1024, num_q_heads=group * hkv)
+        sizes[b, k] = lib.ekv_decode_selected_workspace_bytes(ctypes.byref(pool), ctypes.byref(bt), k)
+    for size in set(sizes.values()):
+        for b, k in itertools.product(BATCHES, (1, 128, 1000)):
+            bt = _batch(batch=b, max_blocks=1024, num_q_heads=group * hkv)
+            a = dict(SELECTED, budget=k, q=AT + 4, ws_bytes=size)   # (refused behind the workspace's check)
+            _refused(lib, lib.ekv_attn_decode_selected(ctypes.byref(pool), ctypes.byref(bt), *a.values(), None), INVALID, "aligned")
+    bt = _batch(batch=1, max_blocks=1024, num_q_heads=group * hkv)
+    _refused(lib, lib.ekv_attn_decode_selected(ctypes.byref(pool), ctypes.byref(bt), *dict(SELECTED, ws_bytes=min(sizes.values()) - 1).values(), None),
+             INVALID, "workspace")
+
+
+@pytest.mark.parametrize("hkv", [1, 3, 8, 64])
+def test_the_binding_s_workspace_has_room_for_smaller_batches_in_full(lib, hkv):  # noqa: F811
+    pool = _pool(num_kv_heads=hkv)
+    for budget in (16, 150, 700):
+        most = 0
+        for b in [*range(1, 70), 96, 128, 129, 256, 257, 384, 385, 600]:
+            batch = _batch(batch=b, num_q_heads=4 * hkv, max_blocks=1024)
+            most = max(most, ekv.decode_selected_workspace_bytes(pool, batch, budget))
+            assert ekv.decode_selected_workspace(pool, batch, budget, device="cpu").numel() >= most
+            assert batch.batch == b

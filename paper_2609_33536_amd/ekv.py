@@ -55,6 +55,7 @@ class Rope(ctypes.Structure):
 class HeadNorm(ctypes.Structure):
     _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("q_stride", ctypes.c_int32),
                 ("k_stride", ctypes.c_int32), ("eps", ctypes.c_float), ("offset", ctypes.c_float)]
+    kinds = (None, None)   # type and heads of the weights, where make_head_norm saw them
 
 
 class CtrlConfig(ctypes.Structure):

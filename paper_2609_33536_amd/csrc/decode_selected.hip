@@ -28,7 +28,9 @@ namespace {
 
 constexpr int kTeam = 4;        // waves of a workgroup
 constexpr int kMostPieces = 64;
-constexpr float kLowest = -3.0e38f;   // reference maximum before the first score: finite, so that -inf scores weigh 0
+// Reference maximum before the first score: finite, so that scores of -inf weigh 0, and the lowest float, so that no finite
+// score lies below it.
+constexpr float kLowest = -0x1.fffffep127f;
 
 // One step's K and V as loaded: 16-bit pools 4 + 4 loads of 16 bytes a block, 8-bit ones
 // 2 of 16 and 4 of 8.  BASE blocks take the same loads, some of them twice the same address

@@ -493,24 +493,16 @@ __global__ __launch_bounds__(64 * WAVES) void join_kernel(SelectArgs a) {
   } else {
     P::each_key(keys, 0, kept, [&](uint64_t k) { seen.add(k); });
   }
-  uint64_t last = 0;
-  int ties = 0;
-  if (n - a.sink - a.recent > need) {
-    P::find_last(keys, 0, kept, need, seen, sm);
-    last = sm.last;
-    ties = sm.ties;
-  } else {
-    __syncthreads();
-  }
+  P::find_last(keys, 0, kept, need, seen, sm);   // (a row that fits the budget has ended above)
   int32_t* out = a.selected + (size_t)row * a.budget + a.sink;
   // (a place beyond `need` only if another call writes this workspace meanwhile)
-  P::list_above(keys, 0, kept, last, ties, sm, [&](int place, int i) {
+  P::list_above(keys, 0, kept, sm.last, sm.ties, sm, [&](int place, int i) {
     if (place < need) out[place] = blocks[i];
   });
 }
 
 // 48 and 144 KiB of LDS.  Keys in LDS are read from there by every step of the pick, which else goes to
-// memory each time; 8 waves are enough for few of them (19 rows of 4 chunks 5.1 us), 16 scan many (one million tokens' 62 chunks 12).
+// memory each time; 8 waves are enough for few of them (19 rows of 4 chunks 5.1 us), 16 scan many (one million tokens' 31 chunks 12.3).
 constexpr int kFewKept = 4096, kManyKept = 12288;
 
 template <typename T, bool F8>

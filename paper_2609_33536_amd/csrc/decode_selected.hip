@@ -494,6 +494,9 @@ hipError_t run_group(const SelectedArgs& a, int group, bool elastic, hipStream_t
 // and what a second workgroup there gains the join costs.  Measured in us, pieces up to 256 | up to 512 workgroups in all,
 // lists of 256 blocks half BASE, 8 KV heads: 16-bit 4 sequences 16.0 | 18.8, 8 22.4 | 32.7, 15 35.8 | 45.3;
 // 8-bit 8 sequences 17.5 | 33.7, 15 24.2 | 34.7.  (8 lists of 256 blocks in 4, 8, 16, 32 pieces: 17.1, 12.6, 10.9, 10.8.)
+// 129 to 255 lists are not cut, though some compute units have none then: uncut | in two | in three pieces, 16-bit 17 sequences
+// 47.2 | 57.7 | 48.0, 20 49.3 | 60.2 | 50.4, 24 53.1 | 63.7 | 67.9, 31 65.6 | 70.1 | 74.7; 8-bit 17 32.8 | 36.4 | 30.7,
+// 24 33.5 | 38.2 | 42.8, 31 35.5 | 41.7 | 50.4.  (16 sequences, in two pieces, 37.6 and 24.1.)
 // Lists of up to 32 blocks take less uncut (9.1, in two pieces 9.6).  A little above 256 lists some compute units
 // have two workgroups and most one: lists of 128 blocks or more are halved up to 384 of them (33 sequences
 // 103.6 -> 87.4, 8-bit 56.5 -> 53.3; 48: 109.6 -> 102.7, 62.6 -> 60.7; but 56: 114.9 -> 124.8, 67.2 -> 76.2).

@@ -10,8 +10,8 @@
 // bound, fixed for all of its loads, so that its share of the query stays in registers.  The partial
 // sums of the 8 loads are summed over the lanes and dealt out to them in one go, half of them a
 // step.  This is bound by HBM: 512 (256) bytes of bounds a block.  32 sequences of 16384 to 32768 16-bit tokens, 8 KV heads:
-// 36.9 us (199 MB, 5.4 TB/s); one of a million 43.2 (256 MB, 5.9 TB/s) and 12.4 for the join; 12 blocks
-// 5.4: a launch and four round trips (lengths, queries and bounds, the pick, the list).
+// 37.3 us (199 MB, 5.3 TB/s); one of a million 43.0 (256 MB, 6.0 TB/s) and 12.0 for the join; 12 blocks
+// 5.6: a launch and four round trips (lengths, queries and bounds, the pick, the list).
 //
 // scan_kernel: a workgroup scores a chunk of a row's blocks into LDS, finds the budget's last score
 // by histograms of what is still in question, and lists the blocks above it in order.  Where a
@@ -502,7 +502,7 @@ __global__ __launch_bounds__(64 * WAVES) void join_kernel(SelectArgs a) {
 }
 
 // 48 and 144 KiB of LDS.  Keys in LDS are read from there by every step of the pick, which else goes to
-// memory each time; 8 waves are enough for few of them (19 rows of 4 chunks 5.1 us), 16 scan many (one million tokens' 31 chunks 12.3).
+// memory each time; 8 waves are enough for few of them (19 rows of 4 chunks 5.1 us), 16 scan many (one million tokens' 31 chunks 12.0).
 constexpr int kFewKept = 4096, kManyKept = 12288;
 
 template <typename T, bool F8>
